@@ -48,7 +48,18 @@ typedef enum {
     PG_EUNAVAIL = 5  /* the mode does not exist for this segment */
 } pg_status;
 
-typedef enum { PG_F32 = 0, PG_BF16 = 1 } pg_dtype;
+/* The last three are operands of the kernels of experts and of 8-bit weights (below) and of no others.  An element is a byte in the 8-bit
+ * types (numel: pg_scaled_weight_bytes, pg_scaled_rows_bytes) and a pair in PG_ROUTED. */
+typedef enum {
+    PG_F32 = 0,
+    PG_BF16 = 1,
+    PG_F8_WEIGHT = 2,  /* experts matrices [n, cols] in e4m3 (4 bits of exponent, 3 of mantissa, no infinity): values [experts, n, Kp], Kp = cols
+                          rounded up to 128, the bytes behind cols zero; then fp32 scales [experts, ceil(n / 128), Kp / 128], one for each
+                          block of 128 x 128.  One allocation. */
+    PG_F8_ROWS = 3,    /* rows of activations in e4m3: values [rows, Kp], the bytes behind cols zero; then scale exponents [rows, Kp / 128
+                          rounded up to 4], a byte e for each 128 values of a row, which stands for 2^(e - 127); the bytes that fill up are 127. */
+    PG_ROUTED = 4      /* {int32 expert, fp32 weight}: a token's slot in front of one expert; an expert below 0: the slot is empty */
+} pg_dtype;
 
 /* The chain's kernels.  fp32 arithmetic inside, one rounding to the storage dtype at the store. */
 typedef enum {
@@ -57,8 +68,42 @@ typedef enum {
     PG_GELU = 2,            /* o[i] = a[i] * Phi(a[i]), Phi the normal CDF (erf form)     */
     PG_RMSNORM = 3,         /* o[r,i] = x[r,i] * rsqrt(mean_i x[r,i]^2 + eps) * g[i]      */
     PG_GEMV = 4,            /* y[r,j] = sum_i W[j,i] * h[r,i]; W row-major [n, cols]      */
-    PG_SCALE_BIAS_RELU = 5  /* o[b,c,p] = max(0, x[b,c,p]*s[c] + b[c]); x is [N,C,inner]  */
+    PG_SCALE_BIAS_RELU = 5, /* o[b,c,p] = max(0, x[b,c,p]*s[c] + b[c]); x is [N,C,inner]  */
+    PG_QUANTIZE = 6,        /* o = x[r,i] in 8 bits, PG_F8_ROWS                           */
+    PG_GEMV_F8 = 7,         /* y[r,j] = sum_i W[j,i] * h[r,i], W in 8 bits, h bf16 or 8 bits */
+    PG_ROUTE = 8,           /* o[r,:] = the n best experts of scores s[r,:], with weights */
+    PG_EXPERT_GEMV = 9,     /* y[r,t,j] = sum_i W[e(r,t)][j,i] * h[r,i] (or h[r,t,i])      */
+    PG_EXPERT_SUM = 10      /* o[r,j] = sum_t w(r,t) * z[r,t,j] (+ x[r,j])                 */
 } pg_op;
+
+/* Kernels of experts and of 8-bit weights: what their fields mean (everything else 0, in[] beyond the listed operands PG_REF_NONE).
+ *
+ * PG_QUANTIZE     in: x [rows, cols], dtype PG_F32 or PG_BF16; out: PG_F8_ROWS; rows, cols, n = cols.  Each 128 values of a row share the
+ *                 scale 2^e, e the least integer of [-126, 127] with max |x| <= 448 * 2^e over the finite x (-126 if all are zero); the
+ *                 value is x * 2^-e, rounded to nearest, ties to even.  What is infinite or not a number becomes not-a-number.
+ * PG_GEMV_F8      in: W PG_F8_WEIGHT of one expert, h [rows, cols] PG_BF16 or PG_F8_ROWS; dtype: of the output, PG_BF16 or PG_F32; rows, n,
+ *                 cols.  Sums in fp32, a block's sum times its scale, one rounding at the store.  With both operands in 8 bits and a bf16
+ *                 output, what the products of eight neighbouring columns have below 2^-13 of the largest of them is dropped; with an fp32
+ *                 output nothing is.  The same holds for PG_EXPERT_GEMV.
+ * PG_ROUTE        in: s [rows, cols], dtype PG_F32 or PG_BF16, and optionally bias [cols] PG_F32 (PG_REF_NONE: zeros); out: PG_ROUTED [rows, n];
+ *                 rows, cols = experts (1 to 1024), n = slots a row (1 to 64, <= cols); m = groups (0 or 1: none; divides cols, <= 64) and
+ *                 inner = how many of them are kept (1 to m); eps = a factor of the weights (0: 1); flags.
+ *                 p = softmax of s over the row, or sigmoid(s) (PG_ROUTE_SIGMOID); experts are compared by c = p + bias, evaluated in 64 bits,
+ *                 equal ones by the lower index.  A group counts as its best c, or as the sum of its two best (PG_ROUTE_GROUP_TOP2); the
+ *                 `inner` best groups stay.  The slots hold the n best experts of those, best first, each with the weight p, divided
+ *                 by the sum of the chosen p (PG_ROUTE_RENORMALIZE; 0 if that is 0), times the factor.  An expert whose score is -infinity or not a
+ *                 number, or whose bias is, is never chosen and counts as nothing; +infinity counts as the largest fp32 number.  Where
+ *                 too few are left, slots are empty: {-1, 0}.
+ * PG_EXPERT_GEMV  in: W PG_BF16 [inner, n, cols] or PG_F8_WEIGHT of `inner` experts, h, r PG_ROUTED [rows, m]; h [rows, cols], or with
+ *                 PG_EXPERT_PER_SLOT [rows, m, cols], PG_BF16 or (with 8-bit W) PG_F8_ROWS; out [rows, m, n], dtype PG_BF16 or PG_F32; m (1 to 64),
+ *                 inner = experts (1 to 1024), rows * m < 2^24.  The rows of a slot whose expert is not one of 0 .. inner - 1 are zero.
+ * PG_EXPERT_SUM   in: z [rows, m, n], r PG_ROUTED [rows, m], and optionally x [rows, n]; dtype of z, x and the output PG_F32 or PG_BF16; rows, n, m (1 to 64).
+ *                 Slots are added in order, x behind them, in fp32; an empty slot's z is not read.  out may be x's buffer.
+ *
+ * An internal PG_F8_ROWS buffer is read with the rows and cols it was last written with.  External 8-bit tensors and weights have exactly the size
+ * of their layout; external pointers to 8-bit tensors are aligned to 16 bytes. */
+enum { PG_ROUTE_SIGMOID = 1, PG_ROUTE_RENORMALIZE = 2, PG_ROUTE_GROUP_TOP2 = 4 };
+enum { PG_EXPERT_PER_SLOT = 1 };
 
 /* Execution variants of a segment; the order is the tie-break order of pg_select. */
 typedef enum { PG_EAGER = 0, PG_GRAPH_COPY = 1, PG_GRAPH_INDIRECT = 2 } pg_mode;
@@ -72,18 +117,18 @@ typedef struct { int32_t dtype; int32_t reserved; int64_t numel; } pg_tensor_des
 
 typedef struct {
     int32_t op;        /* pg_op */
-    int32_t dtype;     /* pg_dtype of every operand and of the output */
+    int32_t dtype;     /* pg_dtype of every operand and of the output (ops up to PG_SCALE_BIAS_RELU; the others: above) */
     int32_t segment;   /* non-decreasing along the chain, starting at 0, no gaps */
     int32_t reserved;
     pg_ref out;        /* must be PG_REF_INT */
-    pg_ref in[3];      /* ADD/MUL: a, b | GELU: a | RMSNORM: x, g | GEMV: W, h | SCALE_BIAS_RELU: x, s, b */
+    pg_ref in[3];      /* ADD/MUL: a, b | GELU: a | RMSNORM: x, g | GEMV: W, h | SCALE_BIAS_RELU: x, s, b | others: above */
     int64_t n;         /* output elements (per row for RMSNORM and GEMV) */
     int64_t m;         /* ADD/MUL: period of b (0 means n); m <= numel(b) */
     int64_t rows;      /* RMSNORM/GEMV: batch rows */
     int64_t cols;      /* GEMV: input width; RMSNORM: hidden size (== n) */
     int64_t inner;     /* SCALE_BIAS_RELU: H*W; channels = numel(s) = numel(b); n % (channels*inner) == 0 */
-    float eps;         /* RMSNORM */
-    int32_t reserved2;
+    float eps;         /* RMSNORM; ROUTE: factor of the weights */
+    int32_t flags;     /* ROUTE, EXPERT_GEMV; not looked at by the ops up to PG_SCALE_BIAS_RELU */
 } pg_kernel_desc;
 
 typedef struct pg_chain pg_chain;
@@ -118,6 +163,11 @@ typedef enum {
     PG_COPY_KERNEL = 0,    /* one batched copy kernel per <= 448 tensors (this library's design)  */
     PG_COPY_MEMCPY = 1     /* one device-to-device hipMemcpyAsync per tensor (the paper's baseline) */
 } pg_copy_refresh;
+
+/* Bytes of a PG_F8_WEIGHT tensor of `experts` matrices [n, cols], and of PG_F8_ROWS [rows, cols].  Host only; -1 for sizes that are not
+ * positive or come to more than 2^40. */
+int64_t pg_scaled_weight_bytes(int64_t experts, int64_t n, int64_t cols);
+int64_t pg_scaled_rows_bytes(int64_t rows, int64_t cols);
 
 /* Bytes of workspace [dev] a chain needs.  Host only.  The descriptor is validated as in
  * pg_chain_build as far as that is possible without the weight descriptors.  ext / ints: [host]

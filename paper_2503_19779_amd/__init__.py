@@ -10,6 +10,13 @@ from .binding import (  # noqa: F401
     select,
     eager_static,
     STATIC_SCRATCH_BYTES,
+    scaled_weight_bytes,
+    scaled_rows_bytes,
+    pack_scaled_weight,
+    ROUTE_SIGMOID,
+    ROUTE_RENORMALIZE,
+    ROUTE_GROUP_TOP2,
+    EXPERT_PER_SLOT,
     version,
     EAGER,
     GRAPH_COPY,

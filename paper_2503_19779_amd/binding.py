@@ -17,8 +17,12 @@ EAGER, GRAPH_COPY, GRAPH_INDIRECT, SELECTED, GRAPH_UPDATE = 0, 1, 2, 3, 4
 TABLE_KERNARG, TABLE_MEMCPY, TABLE_GRAPH_MEMCPY, TABLE_HOST = 0, 1, 2, 3
 COPY_KERNEL, COPY_MEMCPY = 0, 1
 
-_DT = {"f32": 0, "bf16": 1}
-_OP = {"add": 0, "mul": 1, "gelu": 2, "rmsnorm": 3, "gemv": 4, "scale_bias_relu": 5}
+ROUTE_SIGMOID, ROUTE_RENORMALIZE, ROUTE_GROUP_TOP2 = 1, 2, 4      # flags of "route"
+EXPERT_PER_SLOT = 1                                               # of "expert_gemv"
+
+_DT = {"f32": 0, "bf16": 1, "f8_weight": 2, "f8_rows": 3, "routed": 4}
+_OP = {"add": 0, "mul": 1, "gelu": 2, "rmsnorm": 3, "gemv": 4, "scale_bias_relu": 5,
+       "quantize": 6, "gemv_f8": 7, "route": 8, "expert_gemv": 9, "expert_sum": 10}
 _KIND = {"ext": 1, "int": 2, "weight": 3}
 _STATUS = {1: "PG_EINVAL", 2: "PG_ESTATE", 3: "PG_EHIP", 4: "PG_ENOMEM", 5: "PG_EUNAVAIL"}
 
@@ -41,7 +45,7 @@ class _KernelDesc(C.Structure):
     _fields_ = [("op", C.c_int32), ("dtype", C.c_int32), ("segment", C.c_int32), ("reserved", C.c_int32),
                 ("out", _Ref), ("in_", _Ref * 3),
                 ("n", C.c_int64), ("m", C.c_int64), ("rows", C.c_int64), ("cols", C.c_int64), ("inner", C.c_int64),
-                ("eps", C.c_float), ("reserved2", C.c_int32)]
+                ("eps", C.c_float), ("flags", C.c_int32)]
 
 
 class _Stats(C.Structure):
@@ -90,6 +94,10 @@ def lib():
         L.pg_set_dispatch_merge.argtypes = [vp, i32]
         L.pg_set_launched_dispatches.argtypes = [vp, i32]
         L.pg_chain_graph_dispatches.argtypes = [vp, C.POINTER(i32), C.POINTER(i32)]
+        L.pg_scaled_weight_bytes.argtypes = [i64, i64, i64]
+        L.pg_scaled_weight_bytes.restype = i64
+        L.pg_scaled_rows_bytes.argtypes = [i64, i64]
+        L.pg_scaled_rows_bytes.restype = i64
         L.pg_chain_destroy.argtypes = [vp]
         L.pg_chain_destroy.restype = None
         L.pg_last_error.restype = C.c_char_p
@@ -114,6 +122,41 @@ def select(cost) -> np.ndarray:
     out = np.zeros(cost.shape[0], np.uint8)
     _check(lib().pg_select(cost.ctypes.data_as(C.POINTER(C.c_double)), cost.shape[0],
                            out.ctypes.data_as(C.POINTER(C.c_uint8))))
+    return out
+
+
+def _bytes_of(n: int) -> int:
+    if n < 0:
+        raise ValueError("sizes must be positive and come to at most 2^40 bytes")
+    return n
+
+
+def scaled_weight_bytes(experts: int, n: int, cols: int) -> int:
+    """Elements (bytes) of an "f8_weight" tensor of `experts` matrices [n, cols]."""
+    return _bytes_of(lib().pg_scaled_weight_bytes(experts, n, cols))
+
+
+def scaled_rows_bytes(rows: int, cols: int) -> int:
+    """Elements (bytes) of an "f8_rows" tensor [rows, cols]."""
+    return _bytes_of(lib().pg_scaled_rows_bytes(rows, cols))
+
+
+def pack_scaled_weight(values, scales):
+    """An "f8_weight" tensor of a model's 8-bit weights: values [n, cols] or [experts, n, cols] (torch.float8_e4m3fn), scales fp32
+    [(experts,) ceil(n / 128), ceil(cols / 128)].  Done once, when the weights are loaded."""
+    torch = _torch()
+    if values.dtype != torch.float8_e4m3fn or scales.dtype != torch.float32:
+        raise ValueError("values must be float8_e4m3fn, scales float32")
+    if values.dim() == 2:
+        values, scales = values.unsqueeze(0), scales.unsqueeze(0)
+    experts, n, cols = values.shape
+    kb = (cols + 127) // 128
+    if tuple(scales.shape) != (experts, (n + 127) // 128, kb):
+        raise ValueError("one scale for each block of 128 x 128 expected")
+    out = torch.zeros(scaled_weight_bytes(experts, n, cols), dtype=torch.uint8, device=values.device)
+    at = experts * n * kb * 128
+    out[:at].view(experts, n, kb * 128)[..., :cols] = values.view(torch.uint8)
+    out[at:].copy_(scales.contiguous().view(torch.uint8).view(-1))
     return out
 
 
@@ -143,6 +186,7 @@ def pack_descriptor(spec):
             if j < len(k.ins):
                 d.in_[j].kind, d.in_[j].index = _KIND[k.ins[j].kind], k.ins[j].index
         d.n, d.m, d.rows, d.cols, d.inner, d.eps = k.n, k.m, k.rows, k.cols, k.inner, k.eps
+        d.flags = getattr(k, "flags", 0)
 
     def tds(ts):
         arr = (_TensorDesc * max(1, len(ts)))()
@@ -374,7 +418,24 @@ class Chain:
         raw = self.workspace[off:off + nb.value]
         if dtype is None:
             return raw
+        if dtype in ("f8_weight", "f8_rows"):
+            return raw
+        if dtype == "routed":
+            return raw.view(torch.int32).view(-1, 2)
         return raw.view(torch.float32 if dtype == "f32" else torch.bfloat16)
+
+    def routed(self, i: int, rows: int, k: int):
+        """The slots [rows, k] of a "routed" internal buffer: (experts int32, weights float32), views into the workspace."""
+        pairs = self.int_buffer(i)[:rows * k].view(rows, k, 2)
+        return pairs[..., 0], pairs.view(_torch().float32)[..., 1]
+
+    def scaled_rows(self, i: int, rows: int, cols: int):
+        """The rows of an "f8_rows" internal buffer: (values float8_e4m3fn [rows, Kp], scale exponents uint8 [rows, Kp / 128]; a byte e
+        stands for 2^(e - 127)), views into the workspace; Kp = cols rounded up to 128."""
+        raw = self.int_buffer(i)
+        kb = (cols + 127) // 128
+        at, pitch = rows * kb * 128, (kb + 3) // 4 * 4
+        return raw[:at].view(_torch().float8_e4m3fn).view(rows, kb * 128), raw[at:at + rows * pitch].view(rows, pitch)[:, :kb]
 
     def int_buffer(self, i: int):
         return self._view(lib().pg_chain_int_buffer, i, self.spec.ints[i].dtype)
@@ -398,5 +459,5 @@ class Chain:
         return g.value, b.value
 
     def output(self, i: int) -> np.ndarray:
-        """Internal buffer i as numpy (float32, or uint16 bf16 bit patterns); synchronises."""
+        """Internal buffer i as numpy (float32, or uint16 bf16 bit patterns; uint8 bytes, int32 pairs); synchronises."""
         return to_numpy(self.int_buffer(i))

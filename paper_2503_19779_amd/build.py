@@ -8,7 +8,7 @@ import tempfile
 from concurrent.futures import ThreadPoolExecutor
 
 HERE = os.path.dirname(os.path.abspath(__file__))
-SOURCES = [os.path.join(HERE, "csrc", f) for f in ("kernels.hip", "gemv.hip", "chain.hip")]
+SOURCES = [os.path.join(HERE, "csrc", f) for f in ("kernels.hip", "gemv.hip", "experts.hip", "chain.hip")]
 HEADERS = [os.path.join(HERE, "csrc", "kernels.h"), os.path.join(HERE, "csrc", "device.h"), os.path.join(HERE, "..", "include", "pygraph_hip.h"),
            os.path.join(HERE, "..", "include", "pygraph_hip_bench.h")]
 LIB = os.path.join(HERE, "libpygraph_hip.so")

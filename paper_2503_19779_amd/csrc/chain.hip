@@ -51,7 +51,29 @@ pg_status fail(pg_status st, const char* fmt, ...) {
 constexpr size_t kAlign = 256;
 constexpr size_t kNoShadow = ~(size_t)0;
 size_t align_up(size_t x) { return (x + kAlign - 1) / kAlign * kAlign; }
-size_t elem_bytes(int dtype) { return dtype == PG_F32 ? 4 : 2; }
+size_t elem_bytes(int dtype) { return dtype == PG_F32 ? 4 : dtype == PG_BF16 ? 2 : dtype == PG_ROUTED ? sizeof(pgk::Routed) : 1; }
+size_t ext_alignment(int dtype) { return dtype == PG_F8_WEIGHT || dtype == PG_F8_ROWS ? 16 : elem_bytes(dtype); }
+bool known_dtype(int dtype) { return dtype >= PG_F32 && dtype <= PG_ROUTED; }
+
+// Products of sizes that nothing has validated: the largest value for what does not fit
+constexpr long long kTooMany = std::numeric_limits<long long>::max();
+long long times(long long a, long long b) {
+    long long c = 0;
+    return a < 0 || b < 0 || __builtin_mul_overflow(a, b, &c) ? kTooMany : c;
+}
+long long plus(long long a, long long b) {
+    long long c = 0;
+    return a < 0 || b < 0 || __builtin_add_overflow(a, b, &c) ? kTooMany : c;
+}
+long long scale_blocks(long long x) { return plus(x, pgk::kScaleBlock - 1) / pgk::kScaleBlock; }
+long long scaled_weight_bytes(long long experts, long long n, long long cols) {
+    const long long kb = scale_blocks(cols);
+    return times(experts, plus(times(n, times(kb, pgk::kScaleBlock)), times(4, times(scale_blocks(n), kb))));
+}
+long long scaled_rows_bytes(long long rows, long long cols) {
+    const long long kb = scale_blocks(cols);
+    return times(rows, plus(times(kb, pgk::kScaleBlock), plus(kb, 3) / 4 * 4));
+}
 
 union ArgBlock {
     pgk::EwArgs ew;
@@ -59,12 +81,17 @@ union ArgBlock {
     pgk::GemvArgs gemv;
     pgk::GemvAloneArgs alone;       // starts with the GemvArgs; for the GEMV kernels that take the flags as well
     pgk::SbrArgs sbr;
+    pgk::QuantizeArgs quantize;
+    pgk::RouteArgs route;
+    pgk::ExpertArgs expert;
+    pgk::ExpertSumArgs expert_sum;
     // every block starts with: out, in0, in1, (in2)
     const void* ptr[4];
 };
 
 struct KernelRec {
     pgk::Launch direct, indirect;   // same shape, different kernel variant
+    pgk::Launch pre;                // a dispatch in front of it that takes the same argument block, if it has one (fn)
     ArgBlock a_eager, a_copy, a_ind, a_upd;
     ArgBlock a_host[2];             // external operands are slots of the two host-resident tables (PG_TABLE_HOST)
     int n_in = 0;
@@ -132,7 +159,7 @@ struct Segment {
     // host-updated variant: explicit kernel nodes in chain order, two executable instances
     hipGraph_t g_upd = nullptr;
     hipGraphExec_t x_upd[2] = {nullptr, nullptr};
-    std::vector<hipGraphNode_t> nodes;
+    std::vector<hipGraphNode_t> nodes, pre_nodes;     // (pre: of the dispatch in front of the kernel, or null)
     // indirect graphs of the two table mechanisms that alternate between two instances:
     // [0] PG_TABLE_GRAPH_MEMCPY, [1] PG_TABLE_HOST
     hipGraph_t g_alt[2][2] = {{nullptr, nullptr}, {nullptr, nullptr}};
@@ -165,6 +192,7 @@ struct pg_chain {
     char* ws = nullptr;
     size_t ws_bytes = 0, ws_need = 0;
     std::vector<size_t> ph_off, int_off;
+    std::vector<size_t> sorted_off;     // per kernel: where its slots are sorted (PG_EXPERT_GEMV), or kNoShadow
     std::vector<size_t> shadow_off;     // per internal buffer: its second copy (merged dispatches that rename), or kNoShadow
     size_t table_off = 0;
     size_t carry_off = 0;               // two heads that runs with a carry set aside in turn
@@ -199,7 +227,7 @@ namespace {
 
 // ---- descriptor validation and layout ------------------------------------------------------------
 struct Layout {
-    std::vector<size_t> ph_off, int_off, shadow_off;
+    std::vector<size_t> ph_off, int_off, shadow_off, sorted_off;
     size_t table_off = 0, carry_off = 0;
     std::vector<CopyList> lists;
     std::vector<Segment> seg;
@@ -212,7 +240,50 @@ int n_inputs(int op) {
     case PG_ADD: case PG_MUL: case PG_RMSNORM: case PG_GEMV: return 2;
     case PG_GELU: return 1;
     case PG_SCALE_BIAS_RELU: return 3;
+    case PG_QUANTIZE: return 1;
+    case PG_GEMV_F8: case PG_ROUTE: return 2;
+    case PG_EXPERT_GEMV: case PG_EXPERT_SUM: return 3;
     default: return -1;
+    }
+}
+
+// The type operand j may have, beside those of expert_weights' and rows' two (second: or this one); -1: none.
+struct OperandTypes { int first, second; };
+OperandTypes operand_types(const pg_kernel_desc& d, int j) {
+    switch (d.op) {
+    case PG_GEMV_F8: return j == 0 ? OperandTypes{PG_F8_WEIGHT, PG_F8_WEIGHT} : OperandTypes{PG_BF16, PG_F8_ROWS};
+    case PG_ROUTE: return j == 0 ? OperandTypes{d.dtype, d.dtype} : OperandTypes{PG_F32, PG_F32};
+    case PG_EXPERT_GEMV: return j == 0 ? OperandTypes{PG_BF16, PG_F8_WEIGHT} : j == 1 ? OperandTypes{PG_BF16, PG_F8_ROWS} : OperandTypes{PG_ROUTED, PG_ROUTED};
+    case PG_EXPERT_SUM: return j == 1 ? OperandTypes{PG_ROUTED, PG_ROUTED} : OperandTypes{d.dtype, d.dtype};
+    default: return OperandTypes{d.dtype, d.dtype};
+    }
+}
+int out_type(const pg_kernel_desc& d) { return d.op == PG_QUANTIZE ? PG_F8_ROWS : d.op == PG_ROUTE ? PG_ROUTED : d.dtype; }
+bool may_lack(const pg_kernel_desc& d, int j) { return (d.op == PG_ROUTE && j == 1) || (d.op == PG_EXPERT_SUM && j == 2); }
+constexpr long long kMostSlots = 64, kMostExperts = 1024;
+
+// Elements that the kernel writes, and that it reads of operand j
+long long elements_written(const pg_kernel_desc& d) {
+    switch (d.op) {
+    case PG_RMSNORM: return times(d.rows, d.cols);
+    case PG_GEMV: case PG_GEMV_F8: case PG_ROUTE: case PG_EXPERT_SUM: return times(d.rows, d.n);
+    case PG_QUANTIZE: return scaled_rows_bytes(d.rows, d.cols);
+    case PG_EXPERT_GEMV: return times(times(d.rows, d.m), d.n);
+    default: return d.n;
+    }
+}
+long long expert_rows(const pg_kernel_desc& d) { return (d.flags & PG_EXPERT_PER_SLOT) ? times(d.rows, d.m) : d.rows; }
+long long elements_read(const pg_kernel_desc& d, int j, int dtype) {
+    switch (d.op) {
+    case PG_QUANTIZE: return times(d.rows, d.cols);
+    case PG_GEMV_F8: return j == 0 ? scaled_weight_bytes(1, d.n, d.cols) : dtype == PG_F8_ROWS ? scaled_rows_bytes(d.rows, d.cols) : times(d.rows, d.cols);
+    case PG_ROUTE: return j == 0 ? times(d.rows, d.cols) : d.cols;
+    case PG_EXPERT_GEMV:
+        if (j == 2) return times(d.rows, d.m);
+        if (j == 0) return dtype == PG_F8_WEIGHT ? scaled_weight_bytes(d.inner, d.n, d.cols) : times(d.inner, times(d.n, d.cols));
+        return dtype == PG_F8_ROWS ? scaled_rows_bytes(expert_rows(d), d.cols) : times(expert_rows(d), d.cols);
+    case PG_EXPERT_SUM: return j == 0 ? times(times(d.rows, d.m), d.n) : j == 1 ? times(d.rows, d.m) : times(d.rows, d.n);
+    default: return 0;
     }
 }
 
@@ -225,7 +296,7 @@ pg_status validate(const pg_kernel_desc* k, int nk, const pg_tensor_desc* ext, i
     if ((n_ext && !ext) || !ints || (n_w && !w)) return fail(PG_EINVAL, "null tensor descriptor array");
     auto chk_desc = [&](const pg_tensor_desc* d, int n, const char* what) -> pg_status {
         for (int i = 0; i < n; i++) {
-            if (d[i].dtype != PG_F32 && d[i].dtype != PG_BF16) return fail(PG_EINVAL, "%s %d: bad dtype", what, i);
+            if (!known_dtype(d[i].dtype)) return fail(PG_EINVAL, "%s %d: bad dtype", what, i);
             if (d[i].numel <= 0 || d[i].numel > (1ll << 40)) return fail(PG_EINVAL, "%s %d: bad numel", what, i);
         }
         return PG_OK;
@@ -234,6 +305,7 @@ pg_status validate(const pg_kernel_desc* k, int nk, const pg_tensor_desc* ext, i
     if ((st = chk_desc(ext, n_ext, "ext")) || (st = chk_desc(ints, n_int, "int")) || (st = chk_desc(w, n_w, "weight"))) return st;
 
     std::vector<long long> written(n_int, 0);   // elements of each internal buffer written so far
+    std::vector<std::pair<long long, long long>> rows_of(n_int);        // (PG_F8_ROWS) rows and columns it was last written with
     int seg = 0;
     for (int i = 0; i < nk; i++) {
         const pg_kernel_desc& d = k[i];
@@ -245,23 +317,28 @@ pg_status validate(const pg_kernel_desc* k, int nk, const pg_tensor_desc* ext, i
         seg = d.segment;
         if (d.out.kind != PG_REF_INT || d.out.index < 0 || d.out.index >= n_int)
             return fail(PG_EINVAL, "kernel %d: output must be an internal buffer in range", i);
-        if (ints[d.out.index].dtype != d.dtype) return fail(PG_EINVAL, "kernel %d: output dtype mismatch", i);
+        if (ints[d.out.index].dtype != out_type(d)) return fail(PG_EINVAL, "kernel %d: output dtype mismatch", i);
         long long numel_in[3] = {0, 0, 0};
+        int dtype_in[3] = {d.dtype, d.dtype, d.dtype};
         for (int j = 0; j < 3; j++) {
             const pg_ref& r = d.in[j];
             if (j >= nin) {
                 if (r.kind != PG_REF_NONE) return fail(PG_EINVAL, "kernel %d: operand %d must be unused", i, j);
                 continue;
             }
+            if (r.kind == PG_REF_NONE && may_lack(d, j)) continue;
             const pg_tensor_desc* t = nullptr;
             if (r.kind == PG_REF_EXT && r.index >= 0 && r.index < n_ext) t = &ext[r.index];
             else if (r.kind == PG_REF_INT && r.index >= 0 && r.index < n_int) t = &ints[r.index];
             else if (r.kind == PG_REF_WEIGHT && r.index >= 0 && r.index < n_w) t = &w[r.index];
             if (!t) return fail(PG_EINVAL, "kernel %d: operand %d reference out of range", i, j);
-            if (t->dtype != d.dtype) return fail(PG_EINVAL, "kernel %d: operand %d dtype mismatch", i, j);
+            const OperandTypes ok = operand_types(d, j);
+            if (t->dtype != ok.first && t->dtype != ok.second) return fail(PG_EINVAL, "kernel %d: operand %d dtype mismatch", i, j);
+            dtype_in[j] = t->dtype;
             numel_in[j] = t->numel;
             if (r.kind == PG_REF_INT && r.index == d.out.index) {
-                const bool inplace_ok = j == 0 && (d.op == PG_ADD || d.op == PG_MUL || d.op == PG_GELU || d.op == PG_SCALE_BIAS_RELU);
+                const bool inplace_ok = (j == 0 && (d.op == PG_ADD || d.op == PG_MUL || d.op == PG_GELU || d.op == PG_SCALE_BIAS_RELU)) ||
+                                        (j == 2 && d.op == PG_EXPERT_SUM);
                 if (!inplace_ok) return fail(PG_EINVAL, "kernel %d: output overlaps operand %d", i, j);
             }
         }
@@ -295,6 +372,38 @@ pg_status validate(const pg_kernel_desc* k, int nk, const pg_tensor_desc* ext, i
             need[0] = d.n; need[1] = ch; need[2] = ch; out_need = d.n;
             break;
         }
+        default: {
+            if (!fits_i32(d.rows) || !fits_i32(d.n)) return fail(PG_EINVAL, "kernel %d: bad rows/n", i);
+            if (d.op != PG_EXPERT_SUM && !fits_i32(plus(d.cols, pgk::kScaleBlock))) return fail(PG_EINVAL, "kernel %d: bad cols", i);
+            const int flags = d.op == PG_ROUTE ? PG_ROUTE_SIGMOID | PG_ROUTE_RENORMALIZE | PG_ROUTE_GROUP_TOP2 : d.op == PG_EXPERT_GEMV ? PG_EXPERT_PER_SLOT : 0;
+            if (d.flags & ~flags) return fail(PG_EINVAL, "kernel %d: unknown flags", i);
+            if (d.op == PG_QUANTIZE && d.n != d.cols) return fail(PG_EINVAL, "kernel %d: n must equal cols", i);
+            if (d.op == PG_ROUTE) {
+                const long long groups = d.m ? d.m : 1;
+                if (d.cols > kMostExperts || d.n > kMostSlots || d.n > d.cols) return fail(PG_EINVAL, "kernel %d: up to %lld experts, %lld slots a row, no more slots than experts", i, kMostExperts, kMostSlots);
+                if (groups < 1 || groups > kMostSlots || d.cols % groups || (groups > 1 && (d.inner < 1 || d.inner > groups))) return fail(PG_EINVAL, "kernel %d: bad groups", i);
+                if (!std::isfinite(d.eps)) return fail(PG_EINVAL, "kernel %d: the factor of the weights must be finite", i);
+            }
+            if (d.op == PG_EXPERT_GEMV || d.op == PG_EXPERT_SUM) {
+                if (d.m < 1 || d.m > kMostSlots) return fail(PG_EINVAL, "kernel %d: 1 to %lld slots a row", i, kMostSlots);
+                if (times(d.rows, d.m) >= 1ll << 24 && d.op == PG_EXPERT_GEMV) return fail(PG_EINVAL, "kernel %d: rows * m must be below 2^24", i);
+            }
+            if (d.op == PG_EXPERT_GEMV) {
+                if (d.inner < 1 || d.inner > kMostExperts) return fail(PG_EINVAL, "kernel %d: 1 to %lld experts", i, kMostExperts);
+                if (dtype_in[0] == PG_BF16 && dtype_in[1] != PG_BF16) return fail(PG_EINVAL, "kernel %d: 8-bit rows need 8-bit weights", i);
+            }
+            out_need = elements_written(d);
+            for (int j = 0; j < nin; j++) {
+                if (d.in[j].kind == PG_REF_NONE) continue;
+                need[j] = elements_read(d, j, dtype_in[j]);
+                if ((dtype_in[j] == PG_F8_WEIGHT || dtype_in[j] == PG_F8_ROWS) && d.in[j].kind != PG_REF_INT && numel_in[j] != need[j])
+                    return fail(PG_EINVAL, "kernel %d: operand %d has %lld bytes, its layout %lld", i, j, numel_in[j], need[j]);
+                if (dtype_in[j] == PG_F8_ROWS && d.in[j].kind == PG_REF_INT &&
+                    rows_of[d.in[j].index] != std::pair<long long, long long>(d.op == PG_EXPERT_GEMV ? expert_rows(d) : d.rows, d.cols))
+                    return fail(PG_EINVAL, "kernel %d: operand %d was not written with these rows and cols", i, j);
+            }
+            break;
+        }
         }
         if (ints[d.out.index].numel < out_need) return fail(PG_EINVAL, "kernel %d: output buffer too small", i);
         for (int j = 0; j < nin; j++) {
@@ -303,6 +412,7 @@ pg_status validate(const pg_kernel_desc* k, int nk, const pg_tensor_desc* ext, i
                 return fail(PG_EINVAL, "kernel %d: operand %d reads internal buffer %d beyond what earlier kernels wrote", i, j, d.in[j].index);
         }
         written[d.out.index] = std::max(written[d.out.index], out_need);
+        if (d.op == PG_QUANTIZE) rows_of[d.out.index] = {d.rows, d.cols};
     }
     return PG_OK;
 }
@@ -607,14 +717,15 @@ void plan_groups(const pg_kernel_desc* k, int k0, int k1, const pg_tensor_desc* 
 void drop_dead_stores(const pg_kernel_desc* k, int nk, int n_int, std::vector<Segment>& seg, std::vector<Unstored>& unstored) {
     struct Use { int kernel; int operand; long long n; };      // operand -1: writes elements [0, n); else reads them
     std::vector<std::vector<Use>> uses(n_int);
-    auto written = [](const pg_kernel_desc& d) { return d.op == PG_RMSNORM ? (long long)d.rows * d.cols : d.op == PG_GEMV ? (long long)d.rows * d.n : (long long)d.n; };
+    const auto written = elements_written;
     auto read = [](const pg_kernel_desc& d, int j) -> long long {
         switch (d.op) {
         case PG_ADD: case PG_MUL: return j == 0 ? d.n : d.m ? d.m : d.n;
         case PG_RMSNORM: return j == 0 ? (long long)d.rows * d.cols : (long long)d.cols;
         case PG_GEMV: return j == 0 ? (long long)d.n * d.cols : (long long)d.rows * d.cols;
         case PG_GELU: return d.n;
-        default: return j == 0 ? (long long)d.n : std::numeric_limits<long long>::max();      // scale, bias: as long as the buffer
+        case PG_SCALE_BIAS_RELU: return j == 0 ? (long long)d.n : kTooMany;      // scale, bias: as long as the buffer
+        default: return kTooMany;                                               // (none of these rides in a run: whatever it reads is stored)
         }
     };
     for (int i = 0; i < nk; i++) {
@@ -687,6 +798,9 @@ void make_layout(const pg_kernel_desc* k, int nk, const pg_tensor_desc* ext, int
     for (int i = 0; i < n_int; i++) { L.int_off[i] = off; off = align_up(off + (size_t)ints[i].numel * elem_bytes(ints[i].dtype)); }
     L.table_off = off;
     if (!eager_only) off = align_up(off + (size_t)std::max(1, n_ext) * 8);
+    L.sorted_off.assign(nk, kNoShadow);
+    for (int i = 0; i < nk; i++)
+        if (const size_t bytes = pgk::sorted_bytes(k[i].op, shape_of(k[i]))) { L.sorted_off[i] = off; off = align_up(off + bytes); }
     // segments and their external sets
     const int n_seg = k[nk - 1].segment + 1;
     L.seg.assign(n_seg, Segment());
@@ -828,10 +942,42 @@ pg_status make_records(pg_chain* c) {
                 a.sbr.channels = (unsigned)(d.in[1].kind == PG_REF_EXT ? c->ext[d.in[1].index].numel
                                             : d.in[1].kind == PG_REF_INT ? c->ints[d.in[1].index].numel : c->w[d.in[1].index].numel);
                 break;
+            case PG_QUANTIZE:
+                a.quantize.rows = (int)d.rows; a.quantize.cols = (int)d.cols; a.quantize.f32 = d.dtype == PG_F32;
+                a.quantize.slots = mode == 2 ? (unsigned)r.ind_mask : 0u;
+                break;
+            case PG_ROUTE:
+                a.route.rows = (int)d.rows; a.route.experts = (int)d.cols; a.route.k = (int)d.n;
+                a.route.groups = d.m ? (int)d.m : 1; a.route.kept = a.route.groups > 1 ? (int)d.inner : 1;
+                a.route.flags = d.flags; a.route.factor = d.eps != 0.f ? d.eps : 1.f;
+                a.route.slots = mode == 2 ? (unsigned)r.ind_mask : 0u;
+                break;
+            case PG_GEMV_F8: case PG_EXPERT_GEMV: {
+                const bool routed = d.op == PG_EXPERT_GEMV;
+                a.expert.rows = (int)d.rows; a.expert.n = (int)d.n; a.expert.cols = (int)d.cols;
+                a.expert.k = routed ? (int)d.m : 1; a.expert.experts = routed ? (int)d.inner : 1;
+                a.expert.per_slot = routed && (d.flags & PG_EXPERT_PER_SLOT);
+                a.expert.out_f32 = d.dtype == PG_F32;
+                a.expert.sorted = c->sorted_off[i] == kNoShadow ? nullptr : c->ws + c->sorted_off[i];
+                a.expert.slots = mode == 2 ? (unsigned)r.ind_mask : 0u;
+                break;
+            }
+            case PG_EXPERT_SUM:
+                a.expert_sum.rows = (int)d.rows; a.expert_sum.n = (int)d.n; a.expert_sum.k = (int)d.m;
+                a.expert_sum.slots = mode == 2 ? (unsigned)r.ind_mask : 0u;
+                break;
             }
         }
-        const pgk::Shape sh = shape_of(d);
-        if (!pgk::plan(d.op, d.dtype, 0, sh, &r.direct) || !pgk::plan(d.op, d.dtype, r.ind_mask, sh, &r.indirect))
+        pgk::Shape sh = shape_of(d);
+        if (d.op > PG_SCALE_BIAS_RELU) {
+            for (int j = 0; j < 2 && j < r.n_in; j++)
+                if (d.in[j].kind != PG_REF_NONE)
+                    sh.in_dtype[j] = (d.in[j].kind == PG_REF_EXT ? c->ext[d.in[j].index] : d.in[j].kind == PG_REF_INT ? c->ints[d.in[j].index] : c->w[d.in[j].index]).dtype;
+            if (!pgk::plan_experts(d.op, d.dtype, sh, &r.direct, &r.pre)) return fail(PG_EINVAL, "kernel %d: no device kernel for op %d dtype %d", i, d.op, d.dtype);
+            r.indirect = r.direct;
+            if (d.op == PG_GEMV_F8 || d.op == PG_EXPERT_GEMV)
+                for (ArgBlock* a : {&r.a_eager, &r.a_copy, &r.a_ind}) { a->expert.tile = r.direct.tile; a->expert.tiles = r.direct.tiles; }
+        } else if (!pgk::plan(d.op, d.dtype, 0, sh, &r.direct) || !pgk::plan(d.op, d.dtype, r.ind_mask, sh, &r.indirect))
             return fail(PG_EINVAL, "kernel %d: no device kernel for op %d dtype %d", i, d.op, d.dtype);
         if (r.direct.grid.x != r.indirect.grid.x || r.direct.block.x != r.indirect.block.x)
             return fail(PG_EINVAL, "kernel %d: direct and indirect forms disagree on the launch shape", i);
@@ -887,7 +1033,7 @@ pg_status check_call(const pg_chain* c, const void* const* ext, void* stream, bo
     if (n_ext && !ext) return fail(PG_EINVAL, "null external pointer array");
     for (int i = 0; i < n_ext; i++) {
         if (!ext[i]) return fail(PG_EINVAL, "external pointer %d is null", i);
-        if (reinterpret_cast<uintptr_t>(ext[i]) % elem_bytes(c->ext[i].dtype)) return fail(PG_EINVAL, "external pointer %d is not aligned to its element size", i);
+        if (reinterpret_cast<uintptr_t>(ext[i]) % ext_alignment(c->ext[i].dtype)) return fail(PG_EINVAL, "external pointer %d is not aligned to %zu bytes", i, ext_alignment(c->ext[i].dtype));
     }
     return PG_OK;
 }
@@ -897,6 +1043,7 @@ pg_status run_eager_range(pg_chain* c, int k0, int k1, const void* const* ext, h
         KernelRec& r = c->rec[i];
         for (int j = 0; j < r.n_in; j++)
             if (r.ext_of[j] >= 0) r.a_eager.ptr[1 + j] = ext[r.ext_of[j]];
+        if (r.pre.fn) PG_HIP(launch(r.pre, &r.a_eager, s));
         PG_HIP(launch(r.direct, &r.a_eager, s));
     }
     return PG_OK;
@@ -973,6 +1120,7 @@ void destroy_update_graphs(pg_chain* c) {
         if (s.g_upd) (void)hipGraphDestroy(s.g_upd);
         s.g_upd = nullptr;
         s.nodes.clear();
+        s.pre_nodes.clear();
     }
     c->upd_built = false;
     c->upd_used[0] = c->upd_used[1] = false;
@@ -1005,11 +1153,11 @@ void destroy_graphs(pg_chain* c) {
     c->captured = false;
 }
 
-hipKernelNodeParams node_params(KernelRec& r, void** slot) {
+hipKernelNodeParams node_params(KernelRec& r, const pgk::Launch& l, void** slot) {
     hipKernelNodeParams p{};
-    p.func = const_cast<void*>(r.direct.fn);
-    p.gridDim = r.direct.grid;
-    p.blockDim = r.direct.block;
+    p.func = const_cast<void*>(l.fn);
+    p.gridDim = l.grid;
+    p.blockDim = l.block;
     p.sharedMemBytes = 0;
     slot[0] = &r.a_upd;          // every kernel takes its argument block as one by-value struct
     p.kernelParams = slot;
@@ -1025,16 +1173,21 @@ pg_status build_update_graphs(pg_chain* c, hipStream_t s) {
     for (auto& sg : c->seg) {
         PG_HIP(hipGraphCreate(&sg.g_upd, 0));
         sg.nodes.clear();
+        sg.pre_nodes.clear();
         hipGraphNode_t prev = nullptr;
         for (int i = sg.k0; i < sg.k1; i++) {
             KernelRec& r = c->rec[i];
             r.a_upd = r.a_copy;   // external operands start at the placeholders: valid addresses of the right size
             void* slot[1];
-            hipKernelNodeParams p = node_params(r, slot);
-            hipGraphNode_t n = nullptr;
-            PG_HIP(hipGraphAddKernelNode(&n, sg.g_upd, prev ? &prev : nullptr, prev ? 1 : 0, &p));
-            sg.nodes.push_back(n);
-            prev = n;
+            for (const pgk::Launch* l : {&r.pre, &r.direct}) {
+                hipGraphNode_t n = nullptr;
+                if (l->fn) {
+                    hipKernelNodeParams p = node_params(r, *l, slot);
+                    PG_HIP(hipGraphAddKernelNode(&n, sg.g_upd, prev ? &prev : nullptr, prev ? 1 : 0, &p));
+                    prev = n;
+                }
+                (l == &r.pre ? sg.pre_nodes : sg.nodes).push_back(n);
+            }
         }
         for (auto& x : sg.x_upd) {
             PG_HIP(hipGraphInstantiate(&x, sg.g_upd, nullptr, nullptr, 0));
@@ -1060,7 +1213,11 @@ pg_status run_update(pg_chain* c, const void* const* ext, hipStream_t s) {
             for (int j = 0; j < r.n_in; j++)
                 if (r.ext_of[j] >= 0) r.a_upd.ptr[1 + j] = ext[r.ext_of[j]];
             void* slot[1];
-            hipKernelNodeParams p = node_params(r, slot);
+            if (r.pre.fn) {
+                hipKernelNodeParams p = node_params(r, r.pre, slot);
+                PG_HIP(hipGraphExecKernelNodeSetParams(sg.x_upd[which], sg.pre_nodes[i - sg.k0], &p));
+            }
+            hipKernelNodeParams p = node_params(r, r.direct, slot);
             PG_HIP(hipGraphExecKernelNodeSetParams(sg.x_upd[which], sg.nodes[i - sg.k0], &p));
         }
         PG_HIP(hipGraphLaunch(sg.x_upd[which], s));
@@ -1104,6 +1261,7 @@ std::vector<Dispatch> segment_dispatches(pg_chain* c, Segment& sg, int kind, int
             for (int i = grp.k0; i < grp.k1; i++) {
                 KernelRec& r = c->rec[i];
                 const ArgBlock a = versioned(i, nullptr);
+                if (r.pre.fn) emit(r.pre, &a);
                 emit(kind == kGraphCopy ? r.direct : r.indirect, &a);
             }
             continue;
@@ -1458,6 +1616,7 @@ pg_status build_chain(const pg_kernel_desc* kernels, int32_t nk, const pg_tensor
     c->ph_off = std::move(L.ph_off);
     c->int_off = std::move(L.int_off);
     c->shadow_off = std::move(L.shadow_off);
+    c->sorted_off = std::move(L.sorted_off);
     c->table_off = L.table_off;
     c->carry_off = L.carry_off;
     c->copy_lists = std::move(L.lists);
@@ -1504,6 +1663,15 @@ const char* pg_last_error(void) { return g_err.c_str(); }
 int pg_last_hip_error(void) { return g_hip_err; }
 const char* pg_version(void) { return "pygraph_hip 0.1 (gfx950)"; }
 
+int64_t pg_scaled_weight_bytes(int64_t experts, int64_t n, int64_t cols) {
+    const long long b = experts > 0 && n > 0 && cols > 0 ? scaled_weight_bytes(experts, n, cols) : kTooMany;
+    return b > 1ll << 40 ? -1 : b;
+}
+int64_t pg_scaled_rows_bytes(int64_t rows, int64_t cols) {
+    const long long b = rows > 0 && cols > 0 ? scaled_rows_bytes(rows, cols) : kTooMany;
+    return b > 1ll << 40 ? -1 : b;
+}
+
 pg_status pg_chain_workspace_bytes(const pg_kernel_desc* kernels, int32_t nk, const pg_tensor_desc* ext, int32_t n_ext,
                                    const pg_tensor_desc* ints, int32_t n_int, size_t* bytes_out) {
     if (!bytes_out) return fail(PG_EINVAL, "null bytes_out");
@@ -1523,8 +1691,8 @@ pg_status pg_chain_workspace_bytes(const pg_kernel_desc* kernels, int32_t nk, co
                 return fail(PG_EINVAL, "kernel %d: internal reference out of range", i);
         }
     }
-    for (int i = 0; i < n_ext; i++) if (ext[i].numel <= 0 || ext[i].numel > (1ll << 40) || (ext[i].dtype != PG_F32 && ext[i].dtype != PG_BF16)) return fail(PG_EINVAL, "ext %d: bad descriptor", i);
-    for (int i = 0; i < n_int; i++) if (ints[i].numel <= 0 || ints[i].numel > (1ll << 40) || (ints[i].dtype != PG_F32 && ints[i].dtype != PG_BF16)) return fail(PG_EINVAL, "int %d: bad descriptor", i);
+    for (int i = 0; i < n_ext; i++) if (ext[i].numel <= 0 || ext[i].numel > (1ll << 40) || !known_dtype(ext[i].dtype)) return fail(PG_EINVAL, "ext %d: bad descriptor", i);
+    for (int i = 0; i < n_int; i++) if (ints[i].numel <= 0 || ints[i].numel > (1ll << 40) || !known_dtype(ints[i].dtype)) return fail(PG_EINVAL, "int %d: bad descriptor", i);
     Layout L;
     make_layout(kernels, nk, ext, n_ext, ints, n_int, nullptr, nullptr, L);
     *bytes_out = L.total;
@@ -1918,6 +2086,8 @@ pg_status pg_time_kernels(pg_chain* c, const void* const* ext, int32_t k0, int32
         KernelRec& r = c->rec[i];
         for (int j = 0; j < r.n_in; j++)
             if (r.ext_of[j] >= 0) r.a_eager.ptr[1 + j] = ext[r.ext_of[j]];
+        if (r.pre.fn)                                                // (not timed)
+            if (const hipError_t e = launch(r.pre, &r.a_eager, s); e != hipSuccess) { g_hip_err = (int)e; st = fail(PG_EHIP, "kernel launch failed: %s", hipGetErrorString(e)); break; }
         st = launch_timed(r.direct.fn, r.direct.grid, r.direct.block, &r.a_eager, s, evs);
     }
     pg_status st2 = collect_timed(evs, s, dur_us_out, false);

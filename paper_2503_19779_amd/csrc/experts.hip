@@ -1,0 +1,483 @@
+// experts.hip -- routing to experts, the experts' products and their weighted sum, products of 8-bit weights with a scale per block of
+// 128, and the quantisation of rows.  gfx950 only.
+#include "device.h"
+
+#include <algorithm>
+
+namespace pgk {
+namespace {
+
+typedef int v8i __attribute__((ext_vector_type(8)));
+typedef int v4i __attribute__((ext_vector_type(4)));
+typedef __bf16 v8bf __attribute__((ext_vector_type(8)));
+typedef v4u v4u_1 __attribute__((aligned(1)));
+
+template <typename T> __device__ __forceinline__ const T* operand(const void* p, unsigned slots, int j) {
+    return (const T*)resolve_rt(p, (slots >> j) & 1u);
+}
+__device__ __forceinline__ int up_to(int x, int to) { return (x + to - 1) / to * to; }
+
+// ---- PG_QUANTIZE -------------------------------------------------------------------------------------------
+// 16 lanes take a block of 128 values, 8 each; their maximum goes round in four steps of a DPP row.
+__device__ __forceinline__ float row16_max(float v) {
+    v = __builtin_fmaxf(v, dpp_take<0xB1>(v));
+    v = __builtin_fmaxf(v, dpp_take<0x4E>(v));
+    v = __builtin_fmaxf(v, dpp_take<0x141>(v));
+    return __builtin_fmaxf(v, dpp_take<0x140>(v));
+}
+
+template <typename T>
+__global__ __launch_bounds__(kBlock) void k_quantize(QuantizeArgs p) {
+    const T* x = operand<T>(p.x, p.slots, 0);
+    const int nb = (p.cols + kScaleBlock - 1) / kScaleBlock, nb4 = up_to(nb, 4), lane = threadIdx.x & 15;
+    const long long b = (long long)blockIdx.x * (kBlock / 16) + (threadIdx.x >> 4);
+    const bool live = b < (long long)p.rows * nb;
+    const long long row = live ? b / nb : 0;
+    const int kb = live ? (int)(b - row * nb) : 0, c0 = kb * kScaleBlock + lane * 8;
+    float f[8];
+#pragma unroll
+    for (int i = 0; i < 8; i++) f[i] = 0.f;
+    const int left = live ? p.cols - c0 : 0;
+    const T* at = x + row * p.cols + c0;
+#pragma unroll
+    for (int i = 0; i < 8; i++) if (i < left) f[i] = load_elem(at + i);
+    float top = 0.f;
+#pragma unroll
+    for (int i = 0; i < 8; i++) {
+        const float a = __builtin_fabsf(f[i]);
+        top = __builtin_fmaxf(top, a < __builtin_inff() ? a : 0.f);
+    }
+    top = row16_max(top);
+    // 448 = 1.75 * 2^8
+    const unsigned u = __float_as_uint(top);
+    int e = (int)(u >> 23) - 127 - 8 + ((u & 0x7fffffu) > 0x600000u ? 1 : 0);
+    e = e < -126 ? -126 : e;
+    const float by = __uint_as_float((unsigned)(127 - e) << 23);
+    unsigned w[2];
+#pragma unroll
+    for (int i = 0; i < 2; i++) {
+        int q = __builtin_amdgcn_cvt_pk_fp8_f32(f[4 * i] * by, f[4 * i + 1] * by, 0, false);
+        q = __builtin_amdgcn_cvt_pk_fp8_f32(f[4 * i + 2] * by, f[4 * i + 3] * by, q, true);
+        w[i] = (unsigned)q;
+    }
+#pragma unroll
+    for (int i = 0; i < 8; i++)
+        if (!(__builtin_fabsf(f[i]) < __builtin_inff())) w[i / 4] = (w[i / 4] & ~(0xffu << (8 * (i & 3)))) | 0x7fu << (8 * (i & 3));
+    if (!live) return;
+    unsigned char* out = (unsigned char*)p.out;
+    const long long kp = (long long)nb * kScaleBlock;
+    uint2 v;
+    v.x = w[0];
+    v.y = w[1];
+    *(uint2*)(out + row * kp + c0) = v;
+    unsigned char* scales = out + (long long)p.rows * kp + row * nb4;
+    if (lane == 0) scales[kb] = (unsigned char)(e + 127);
+    if (kb == nb - 1 && lane >= 1 && nb - 1 + lane < nb4) scales[nb - 1 + lane] = 127;
+}
+
+// ---- PG_EXPERT_SUM -----------------------------------------------------------------------------------------
+template <typename T>
+__global__ __launch_bounds__(kBlock) void k_expert_sum(ExpertSumArgs p) {
+    const T* z = operand<T>(p.z, p.slots, 0);
+    const Routed* r = operand<Routed>(p.r, p.slots, 1);
+    const T* x = p.x ? operand<T>(p.x, p.slots, 2) : nullptr;
+    const long long i = (long long)blockIdx.x * kBlock + threadIdx.x;
+    if (i >= (long long)p.rows * p.n) return;
+    const long long row = i / p.n;
+    const int j = (int)(i - row * p.n);
+    float acc = 0.f;
+    for (int t = 0; t < p.k; t++) {
+        const Routed q = r[row * p.k + t];
+        if (q.expert >= 0) acc = __builtin_fmaf(q.weight, load_elem(z + (row * p.k + t) * p.n + j), acc);
+    }
+    if (x) acc += load_elem(x + i);
+    store_elem((T*)p.out + i, acc);
+}
+
+// ---- PG_ROUTE ----------------------------------------------------------------------------------------------
+__device__ __forceinline__ double dmax(double a, double b) { return a > b ? a : b; }
+template <int CTRL> __device__ __forceinline__ double dpp_take64(double v) {
+    const unsigned long long u = __builtin_bit_cast(unsigned long long, v);
+    const unsigned lo = (unsigned)__builtin_amdgcn_update_dpp(0, (int)(unsigned)u, CTRL, 0xf, 0xf, false);
+    const unsigned hi = (unsigned)__builtin_amdgcn_update_dpp(0, (int)(unsigned)(u >> 32), CTRL, 0xf, 0xf, false);
+    return __builtin_bit_cast(double, (unsigned long long)hi << 32 | lo);
+}
+__device__ __forceinline__ double read_lane64(double v, int lane) {
+    const unsigned long long u = __builtin_bit_cast(unsigned long long, v);
+    const unsigned lo = (unsigned)__builtin_amdgcn_readlane((int)(unsigned)u, lane), hi = (unsigned)__builtin_amdgcn_readlane((int)(unsigned)(u >> 32), lane);
+    return __builtin_bit_cast(double, (unsigned long long)hi << 32 | lo);
+}
+template <class Op> __device__ __forceinline__ double wave_all64(double v, Op op) {
+    v = op(v, dpp_take64<0xB1>(v));
+    v = op(v, dpp_take64<0x4E>(v));
+    v = op(v, dpp_take64<0x141>(v));
+    v = op(v, dpp_take64<0x140>(v));
+    return op(op(read_lane64(v, 0), read_lane64(v, 16)), op(read_lane64(v, 32), read_lane64(v, 48)));
+}
+
+// A wave takes a row, lane l the experts l, l + 64, ...
+template <typename T, int V>
+__global__ __launch_bounds__(kBlock) void k_route(RouteArgs p) {
+    __shared__ double keys[kBlock / 64][V * 64];
+    const T* s = operand<T>(p.s, p.slots, 0);
+    const float* bias = p.bias ? operand<float>(p.bias, p.slots, 1) : nullptr;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int row = blockIdx.x * (kBlock / 64) + wave;
+    const bool live = row < p.rows;
+    const T* sr = s + (long long)(live ? row : 0) * p.experts;
+    const double none = -__builtin_inf();
+    double x[V], key[V], pr[V];
+    bool ok[V];
+    double top = none;
+#pragma unroll
+    for (int i = 0; i < V; i++) {
+        const int e = lane + 64 * i;
+        const float f = e < p.experts ? load_elem(sr + e) : -__builtin_inff();
+        ok[i] = f > -__builtin_inff();
+        x[i] = (double)__builtin_fminf(f, 3.40282347e38f);
+        if (ok[i]) top = dmax(top, x[i]);
+    }
+    top = wave_all64(top, dmax);
+    double total = 0.;
+#pragma unroll
+    for (int i = 0; i < V; i++) {
+        pr[i] = 0.;
+        if (ok[i]) pr[i] = (p.flags & 1) ? 1. / (1. + exp(-x[i])) : exp(x[i] - top);
+        total += pr[i];
+    }
+    if (!(p.flags & 1)) {
+        total = wave_all64(total, [](double a, double b) { return a + b; });
+#pragma unroll
+        for (int i = 0; i < V; i++) if (ok[i]) pr[i] = pr[i] / total;
+    }
+#pragma unroll
+    for (int i = 0; i < V; i++) {
+        const int e = lane + 64 * i;
+        double c = x[i];
+        if (bias && e < p.experts) c = pr[i] + (double)bias[e];
+        key[i] = ok[i] && c > none ? c : none;
+    }
+    if (p.groups > 1) {
+        const int per = p.experts / p.groups;
+        const bool two = (p.flags & 4) != 0;
+#pragma unroll
+        for (int i = 0; i < V; i++) keys[wave][lane + 64 * i] = key[i] > none ? (two && !bias ? pr[i] : key[i]) : none;
+        __syncthreads();
+        double best = none, second = none;
+        if (lane < p.groups)
+            for (int i = 0; i < per; i++) {
+                const double v = keys[wave][lane * per + i];
+                if (v > best) { second = best; best = v; }
+                else if (v > second) second = v;
+            }
+        if (two && second > none) best += second;
+        int before = 0;                // groups that come before this one
+        for (int g = 0; g < p.groups; g++) {
+            const double v = read_lane64(best, g);
+            before += v > best || (v == best && g < lane);
+        }
+        const unsigned long long kept = __ballot(lane < p.groups && before < p.kept);
+#pragma unroll
+        for (int i = 0; i < V; i++) {
+            const int e = lane + 64 * i;
+            if (e < p.experts && !((kept >> (e / per)) & 1ull)) key[i] = none;
+        }
+    }
+    int mine = -1;
+    double weight = 0., sum = 0.;
+    for (int t = 0; t < p.k; t++) {
+        double best = key[0];
+#pragma unroll
+        for (int i = 1; i < V; i++) best = dmax(best, key[i]);
+        best = wave_all64(best, dmax);
+        if (!(best > none)) break;
+        bool found = false;
+#pragma unroll
+        for (int i = 0; i < V; i++) {
+            const unsigned long long at = __ballot(!found && key[i] == best);
+            if (at) {
+                const int l = __builtin_ctzll(at);
+                const double w = read_lane64(pr[i], l);
+                if (lane == t) { mine = l + 64 * i; weight = w; }
+                if (lane == l) key[i] = none;
+                sum += w;
+                found = true;
+            }
+        }
+    }
+    if (p.flags & 2) weight = sum > 0. ? weight / sum : 0.;
+    if (live && lane < p.k) {
+        Routed q;
+        q.expert = mine;
+        q.weight = (float)(weight * (double)p.factor);
+        ((Routed*)p.out)[(long long)row * p.k + lane] = q;
+    }
+}
+
+// ---- PG_EXPERT_GEMV: the slots in the order of their experts ---------------------------------------------------
+constexpr int kSortWaves = 8, kSortMostExperts = 1024;
+__device__ __forceinline__ SortedTile* sorted_tiles(void* area) { return (SortedTile*)((SortedSlots*)area + 1); }
+__device__ __forceinline__ int* sorted_order(void* area, int tiles) { return (int*)(sorted_tiles(area) + tiles); }
+
+// One workgroup.  Each wave takes a stretch of the slots, 64 at a time: lanes of one expert find each other by a ballot for each bit of its
+// number.  First how many of each expert a wave has, then from those counts where its first one goes, then the slots to their places:
+// the order is the slots' own, whatever the waves' pace.  Bucket `experts` takes the empty slots.
+__device__ __forceinline__ unsigned long long same_bucket(int id, int bits) {
+    unsigned long long m = ~0ull;
+    for (int b = 0; b < bits; b++) {
+        const unsigned long long on = __ballot((id >> b) & 1);
+        m &= ((id >> b) & 1) ? on : ~on;
+    }
+    return m;
+}
+__global__ __launch_bounds__(kSortWaves * 64) void k_sort_slots(ExpertArgs p) {
+    __shared__ int cnt[kSortWaves][kSortMostExperts + 1];
+    __shared__ int wave_slots[kSortWaves], wave_tiles[kSortWaves];
+    const Routed* r = operand<Routed>(p.r, p.slots, 2);
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, buckets = p.experts + 1;
+    const int slots = p.rows * p.k, stretch = (slots + kSortWaves * 64 - 1) / (kSortWaves * 64) * 64;
+    const int s0 = wave * stretch, s1 = s0 + stretch < slots ? s0 + stretch : slots;
+    const int bits = 32 - __builtin_clz(p.experts);
+    for (int i = tid; i < kSortWaves * (kSortMostExperts + 1); i += kSortWaves * 64) (&cnt[0][0])[i] = 0;
+    __syncthreads();
+    auto bucket_of = [&](int s) {
+        const int e = s < s1 ? r[s].expert : 0;
+        return (unsigned)e < (unsigned)p.experts ? e : p.experts;
+    };
+    for (int at = s0; at < s1; at += 64) {
+        const int s = at + lane, id = bucket_of(s);
+        const unsigned long long live = __ballot(s < s1), m = same_bucket(id, bits) & live;
+        if (s < s1 && lane == __builtin_ctzll(m)) cnt[wave][id] += __popcll(m);
+    }
+    __syncthreads();
+    // slots and tiles in front of each bucket: a thread takes three neighbouring buckets (1025 of 512 threads)
+    constexpr int kPer = (kSortMostExperts + 1 + kSortWaves * 64 - 1) / (kSortWaves * 64);
+    int c[kPer], n_slots = 0, n_tiles = 0;
+    for (int q = 0; q < kPer; q++) {
+        const int b = tid * kPer + q;
+        c[q] = 0;
+        if (b < buckets) for (int w = 0; w < kSortWaves; w++) c[q] += cnt[w][b];
+        n_slots += c[q];
+        n_tiles += (c[q] + p.tile - 1) / p.tile;
+    }
+    int slots_before = n_slots, tiles_before = n_tiles;
+    for (int d = 1; d < 64; d <<= 1) {
+        const int a = __shfl_up(slots_before, d), b = __shfl_up(tiles_before, d);
+        if (lane >= d) { slots_before += a; tiles_before += b; }
+    }
+    if (lane == 63) { wave_slots[wave] = slots_before; wave_tiles[wave] = tiles_before; }
+    slots_before -= n_slots;
+    tiles_before -= n_tiles;
+    __syncthreads();
+    int all = 0;
+    for (int w = 0; w < kSortWaves; w++) {
+        if (w < wave) { slots_before += wave_slots[w]; tiles_before += wave_tiles[w]; }
+        all += wave_tiles[w];
+    }
+    SortedTile* tiles = sorted_tiles(p.sorted);
+    for (int q = 0; q < kPer; q++) {
+        const int b = tid * kPer + q;
+        if (b >= buckets) break;
+        for (int i = 0; i < c[q]; i += p.tile)
+            tiles[tiles_before++] = SortedTile{b < p.experts ? b : -1, slots_before + i, slots_before + (i + p.tile < c[q] ? i + p.tile : c[q]), 0};
+        int base = slots_before;
+        for (int w = 0; w < kSortWaves; w++) { const int n = cnt[w][b]; cnt[w][b] = base; base += n; }
+        slots_before += c[q];
+    }
+    if (tid == 0) ((SortedSlots*)p.sorted)->n_tiles = all;
+    __syncthreads();
+    int* order = sorted_order(p.sorted, p.tiles);
+    for (int at = s0; at < s1; at += 64) {
+        const int s = at + lane, id = bucket_of(s);
+        const unsigned long long live = __ballot(s < s1), m = same_bucket(id, bits) & live;
+        if (s < s1) {
+            const int base = cnt[wave][id];
+            order[base + __popcll(m & ((1ull << lane) - 1ull))] = s;
+            if (lane == __builtin_ctzll(m)) cnt[wave][id] = base + __popcll(m);
+        }
+    }
+}
+
+// ---- products ----------------------------------------------------------------------------------------------
+// Eight bf16 values of a row from column c on, zeros beyond its last one
+__device__ __forceinline__ v4u row8(const bf16_t* row, int c, int cols) {
+    v4u v = {0u, 0u, 0u, 0u};
+    if (c + 8 <= cols) {
+        v = *(const v4u_any PG_GLOBAL*)(uintptr_t)(row + c);
+    } else {
+        unsigned w[4] = {0u, 0u, 0u, 0u};
+#pragma unroll
+        for (int i = 0; i < 8; i++) if (c + i < cols) w[i / 2] |= (unsigned)row[c + i] << (16 * (i & 1));
+        v.x = w[0]; v.y = w[1]; v.z = w[2]; v.w = w[3];
+    }
+    return v;
+}
+__device__ __forceinline__ v4u bytes16(const unsigned char* p) { return *(const v4u PG_GLOBAL*)(uintptr_t)p; }
+template <bool HI> __device__ __forceinline__ unsigned f8_to_bf16(unsigned w) {
+    return __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, 1.0f, HI));
+}
+// eight e4m3 values (two words) as bf16: exact
+__device__ __forceinline__ v4u f8x8_to_bf16(unsigned a, unsigned b) {
+    v4u v;
+    v.x = f8_to_bf16<false>(a); v.y = f8_to_bf16<true>(a); v.z = f8_to_bf16<false>(b); v.w = f8_to_bf16<true>(b);
+    return v;
+}
+__device__ __forceinline__ v4u half_to_bf16(v4u v, int high) { return high ? f8x8_to_bf16(v.z, v.w) : f8x8_to_bf16(v.x, v.y); }
+__device__ __forceinline__ f32x4 mfma_bf16(v4u a, v4u b, f32x4 c) {
+    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(v8bf, a), __builtin_bit_cast(v8bf, b), c, 0, 0, 0);
+}
+
+// What the operands are.  8-bit rows go two ways.  The 8-bit matrix instruction lines up the products of eight neighbouring columns with the
+// largest of them and drops what lies below 2^-13 of its binade (found with one large and one small product at every pair of places; between
+// the groups, and onto the accumulator, it adds in fp32): rms 1.5e-5 to 5e-5 of the result, which a bf16 output with its half step of 2^-8 does not
+// show.  An fp32 output would, so there both operands become bf16, exactly, and the bf16 instruction, which sums in fp32, takes them.
+enum Form : int { kW16H16, kW8H16, kW8H8, kW8H8Wide };
+
+// A workgroup: 16 outputs of up to 16 rows of h; its four waves take the blocks of 128 columns in turn.
+template <Form FORM, bool ROUTED>
+__global__ __launch_bounds__(kBlock) void k_product(ExpertArgs p) {
+    constexpr bool W8 = FORM != kW16H16, H8 = FORM == kW8H8 || FORM == kW8H8Wide;
+    __shared__ float part[4][16][17];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, l16 = lane & 15, quad = lane >> 4;
+    const int jt = (p.n + 15) / 16;
+    const int t = (int)(blockIdx.x / (unsigned)jt), j0 = (int)(blockIdx.x % (unsigned)jt) * 16;
+    int expert = 0, begin = t * 16, end = begin + 16 < p.rows ? begin + 16 : p.rows;
+    const int* order = nullptr;
+    if constexpr (ROUTED) {
+        if (t >= ((const SortedSlots*)p.sorted)->n_tiles) return;
+        const SortedTile st = sorted_tiles(p.sorted)[t];
+        expert = st.expert;
+        begin = st.begin;
+        end = st.end;
+        order = sorted_order(p.sorted, p.tiles);
+    }
+    auto slot_of = [&](int i) { return ROUTED ? order[begin + i] : begin + i; };      // the i-th slot of the tile
+    const int used = end - begin;
+    f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+    const int nb = (p.cols + kScaleBlock - 1) / kScaleBlock;
+    const long long kp = (long long)nb * kScaleBlock;
+    if (!ROUTED || expert >= 0) {
+        const int j = j0 + l16 < p.n ? j0 + l16 : p.n - 1;
+        const int slot = slot_of(l16 < used ? l16 : used - 1);
+        const long long hrow = ROUTED && !p.per_slot ? slot / p.k : slot;
+        const int hrows = ROUTED && p.per_slot ? p.rows * p.k : p.rows;
+        const unsigned char* w8 = operand<unsigned char>(p.W, p.slots, 0);
+        const float* scales = (const float*)(w8 + (long long)p.experts * p.n * kp) + ((long long)expert * ((p.n + kScaleBlock - 1) / kScaleBlock) + j0 / kScaleBlock) * nb;
+        const bf16_t* w16 = (const bf16_t*)w8 + ((long long)expert * p.n + j) * p.cols;
+        w8 += ((long long)expert * p.n + j) * kp;
+        const unsigned char* h8 = operand<unsigned char>(p.h, p.slots, 1);
+        const bf16_t* h16 = (const bf16_t*)h8 + hrow * p.cols;
+        const unsigned char* hs = h8 + hrows * kp + hrow * up_to(nb, 4);
+        h8 += hrow * kp;
+        for (int kb = wave; kb < nb; kb += 4) {
+            // a lane's 32 of the block's 128 columns: 16 at quad * 16 and 16 at 64 + quad * 16
+            f32x4 sum = {0.f, 0.f, 0.f, 0.f};
+            const int c0 = kb * kScaleBlock + quad * 16;
+            v4u a[2];
+            if constexpr (W8) {
+                a[0] = bytes16(w8 + c0);
+                a[1] = bytes16(w8 + c0 + 64);
+            }
+            v4u b[2];
+            if constexpr (FORM == kW8H8Wide) {
+                b[0] = bytes16(h8 + c0);
+                b[1] = bytes16(h8 + c0 + 64);
+            }
+            if constexpr (FORM == kW8H8) {
+                const v4u b0 = bytes16(h8 + c0), b1 = bytes16(h8 + c0 + 64);
+                const v8i A = {(int)a[0].x, (int)a[0].y, (int)a[0].z, (int)a[0].w, (int)a[1].x, (int)a[1].y, (int)a[1].z, (int)a[1].w};
+                const v8i B = {(int)b0.x, (int)b0.y, (int)b0.z, (int)b0.w, (int)b1.x, (int)b1.y, (int)b1.z, (int)b1.w};
+                sum = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(A, B, sum, 0, 0, 0, 127, 0, (int)hs[kb]);
+            } else {
+#pragma unroll
+                for (int q = 0; q < 4; q++) {
+                    const int c = c0 + (q >> 1) * 64 + (q & 1) * 8;
+                    const v4u A = W8 ? half_to_bf16(a[q >> 1], q & 1) : row8(w16, c, p.cols);
+                    sum = mfma_bf16(A, H8 ? half_to_bf16(b[q >> 1], q & 1) : row8(h16, c, p.cols), sum);
+                }
+            }
+            float s = W8 ? scales[kb] : 1.f;
+            if constexpr (FORM == kW8H8Wide) s = __builtin_ldexpf(s, (int)hs[kb] - 127);
+#pragma unroll
+            for (int i = 0; i < 4; i++) acc[i] = W8 ? __builtin_fmaf(s, sum[i], acc[i]) : acc[i] + sum[i];
+        }
+    }
+#pragma unroll
+    for (int i = 0; i < 4; i++) part[wave][l16][quad * 4 + i] = acc[i];
+    __syncthreads();
+    const int m = threadIdx.x >> 4, c = threadIdx.x & 15;
+    if (m < used && j0 + c < p.n) {
+        const float y = (part[0][m][c] + part[1][m][c]) + (part[2][m][c] + part[3][m][c]);
+        const long long at = (long long)slot_of(m) * p.n + j0 + c;
+        if (p.out_f32) ((float*)p.out)[at] = y;
+        else ((bf16_t*)p.out)[at] = (bf16_t)f32_to_bf16(y);
+    }
+}
+
+template <typename T> const void* route_kernel(int experts) {
+    return experts <= 64 ? PG_FN(k_route<T, 1>) : experts <= 128 ? PG_FN(k_route<T, 2>) : experts <= 256 ? PG_FN(k_route<T, 4>) : experts <= 512 ? PG_FN(k_route<T, 8>)
+                         : PG_FN(k_route<T, 16>);
+}
+
+constexpr long long kSmallestTile = 16;
+long long most_tiles(long long slots, long long experts, long long tile) { return slots / tile + std::min(slots, experts + 1); }
+
+}  // namespace
+
+size_t sorted_bytes(int op, const Shape& s) {
+    if (op != kExpertGemv || s.rows < 1 || s.m < 1 || s.m > (1 << 24) / s.rows || s.inner < 1 || s.inner > kSortMostExperts) return 0;
+    const long long slots = s.rows * s.m;
+    return sizeof(SortedSlots) + (size_t)most_tiles(slots, s.inner, kSmallestTile) * sizeof(SortedTile) + (size_t)slots * sizeof(int);
+}
+
+bool plan_experts(int op, int dtype, const Shape& s, Launch* out, Launch* pre) {
+    *out = Launch();
+    *pre = Launch();
+    out->block = dim3(kBlock);
+    const bool f32 = dtype == kF32;
+    switch (op) {
+    case kQuantize: {
+        const long long blocks = s.rows * ((s.cols + kScaleBlock - 1) / kScaleBlock);
+        if (blocks > (1ll << 34)) return false;
+        out->fn = f32 ? PG_FN(k_quantize<float>) : PG_FN(k_quantize<bf16_t>);
+        out->arg_bytes = sizeof(QuantizeArgs);
+        out->grid = dim3(blocks_for(blocks, kBlock / 16));
+        return true;
+    }
+    case kRoute:
+        out->fn = f32 ? route_kernel<float>((int)s.cols) : route_kernel<bf16_t>((int)s.cols);
+        out->arg_bytes = sizeof(RouteArgs);
+        out->grid = dim3(blocks_for(s.rows, kBlock / 64));
+        return true;
+    case kExpertSum:
+        if (s.rows * s.n > (1ll << 38)) return false;
+        out->fn = f32 ? PG_FN(k_expert_sum<float>) : PG_FN(k_expert_sum<bf16_t>);
+        out->arg_bytes = sizeof(ExpertSumArgs);
+        out->grid = dim3(blocks_for(s.rows * s.n, kBlock));
+        return true;
+    case kGemvF8: case kExpertGemv: {
+        const bool routed = op == kExpertGemv, w8 = s.in_dtype[0] == kF8Weight, h8 = s.in_dtype[1] == kF8Rows;
+        const long long slots = routed ? s.rows * s.m : s.rows;
+        out->tile = (int)kSmallestTile;
+        const long long tiles = routed ? most_tiles(slots, s.inner, out->tile) : (slots + out->tile - 1) / out->tile;
+        out->tiles = (int)tiles;
+        const long long grid = tiles * ((s.n + 15) / 16);
+        if (grid > 0x7fffffffll) return false;
+        out->arg_bytes = sizeof(ExpertArgs);
+        out->grid = dim3((unsigned)grid);
+        const Form form = !w8 ? kW16H16 : !h8 ? kW8H16 : f32 ? kW8H8Wide : kW8H8;
+        out->fn = routed ? (form == kW16H16 ? PG_FN(k_product<kW16H16, true>) : form == kW8H16 ? PG_FN(k_product<kW8H16, true>)
+                            : form == kW8H8 ? PG_FN(k_product<kW8H8, true>) : PG_FN(k_product<kW8H8Wide, true>))
+                         : (form == kW8H16 ? PG_FN(k_product<kW8H16, false>) : form == kW8H8 ? PG_FN(k_product<kW8H8, false>) : PG_FN(k_product<kW8H8Wide, false>));
+        if (routed) {
+            pre->fn = PG_FN(k_sort_slots);
+            pre->arg_bytes = sizeof(ExpertArgs);
+            pre->block = dim3(kSortWaves * 64);
+        }
+        return true;
+    }
+    default: return false;
+    }
+}
+
+}  // namespace pgk

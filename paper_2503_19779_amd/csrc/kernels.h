@@ -7,8 +7,9 @@
 
 namespace pgk {
 
-enum Op : int { kAdd = 0, kMul = 1, kGelu = 2, kRmsNorm = 3, kGemv = 4, kScaleBiasRelu = 5 };
-enum DType : int { kF32 = 0, kBF16 = 1 };
+enum Op : int { kAdd = 0, kMul = 1, kGelu = 2, kRmsNorm = 3, kGemv = 4, kScaleBiasRelu = 5,
+                kQuantize = 6, kGemvF8 = 7, kRoute = 8, kExpertGemv = 9, kExpertSum = 10 };
+enum DType : int { kF32 = 0, kBF16 = 1, kF8Weight = 2, kF8Rows = 3, kRouted = 4 };
 
 // One argument block per kernel, passed by value as the kernel's single parameter.  An operand
 // whose bit is set in the kernel's IND template mask holds the address of a pointer-table slot
@@ -47,6 +48,62 @@ struct SbrArgs {
     unsigned inner;
     unsigned channels;
 };
+
+// The kernels of experts and of 8-bit weights (experts.hip) decide at run time what holds a pointer-table slot: bit j of `slots` for operand j.
+constexpr int kScaleBlock = 128;         // values that share a scale
+struct Routed { int expert; float weight; };
+struct QuantizeArgs {
+    void* out;
+    const void* x;
+    unsigned slots;
+    int rows;
+    int cols;
+    int f32;             // x is fp32, else bf16
+};
+struct RouteArgs {
+    void* out;
+    const void* s;
+    const void* bias;    // may be null
+    unsigned slots;
+    int rows;
+    int experts;
+    int k;
+    int groups;
+    int kept;
+    int flags;           // pg_op's flags
+    float factor;
+};
+struct ExpertArgs {      // kGemvF8, kExpertGemv
+    void* out;
+    const void* W;
+    const void* h;
+    const void* r;       // Routed [rows, k]; null: every row is the one expert's
+    void* sorted;        // SortedSlots in the workspace, or null
+    unsigned slots;
+    int rows;            // of h that belong to the rows of r
+    int n;
+    int cols;
+    int k;               // slots a row; 1 without r
+    int experts;
+    int per_slot;        // h has a row for each slot
+    int out_f32;
+    int tile;            // slots of a tile; from Launch
+    int tiles;           // tiles of the grid at most; from Launch
+};
+struct ExpertSumArgs {
+    void* out;
+    const void* z;
+    const void* r;
+    const void* x;       // may be null
+    unsigned slots;
+    int rows;
+    int n;
+    int k;
+};
+// The slots of a PG_EXPERT_GEMV in the order of their experts (the empty ones last), cut into tiles that have one expert each: a header, then Tile[tiles], then
+// int[slots].  Written by a dispatch of its own in front of the products.
+struct SortedSlots { int n_tiles; int reserved[3]; };
+struct SortedTile { int expert; int begin; int end; int reserved; };     // of `order`; expert -1: rows of zeros
 
 // Batched multi-tensor copy: the destination side is static and lives in device memory, the
 // source pointers change every replay and travel in the argument block.
@@ -224,6 +281,7 @@ struct Launch {
     unsigned arg_bytes = 0;          // size of the kernel's argument block
     dim3 grid{1, 1, 1};
     dim3 block{1, 1, 1};
+    int tile = 0, tiles = 0;         // experts.hip: slots a tile, tiles
     unsigned gemm_row_groups = 0;    // GEMV on the matrix cores: goes into GemvArgs::row_groups (0 = other kernels); k_gemm_rows: tiles of rows | (65536 / tiles, rounded up) << 8
     const void* fn_beyond_cache = nullptr;      // ... and the kernel that takes its weights by non-temporal loads, where the chain settles that (settle_weights)
 };
@@ -237,6 +295,7 @@ inline void settle_weights(Launch* l, long long chain_weight_bytes) {
 
 struct Shape {
     long long n = 0, m = 0, rows = 1, cols = 0, inner = 0;
+    int in_dtype[2] = {kBF16, kBF16};       // kGemvF8, kExpertGemv: of W and h
 };
 
 // Kernel instantiation and launch shape for (op, dtype, mask of indirected operands, shape).  The
@@ -246,6 +305,10 @@ bool plan(int op, int dtype, int ind_mask, const Shape& shape, Launch* out);
 bool plan_gemv(int dtype, int ind_mask, int rows, int n, int cols, Launch* out);    // its part for kGemv (gemv.hip)
 const void* copy_kernel();
 const void* table_kernel();
+// The kernels of experts.hip.  in front of the launch of a kExpertGemv another one may go that sorts its slots: *pre (fn null: none).
+bool plan_experts(int op, int dtype, const Shape& shape, Launch* out, Launch* pre);
+// Bytes of workspace that sorting takes (0: none).  The sizes need not have been validated.
+size_t sorted_bytes(int op, const Shape& shape);
 // Can this kernel be part of a merged dispatch?  From op, dtype and shape alone.  On success *n_out is
 // the number of elements it produces (all kernels of a run must agree on it and on the dtype).
 // whole_vectors: fp32 tensors must be a whole number of 16-byte vectors (runs of one workgroup per unit; a GEMV's

@@ -11,9 +11,9 @@ from typing import List, Optional, Tuple
 
 EXT, INT, WEIGHT = "ext", "int", "weight"
 
-OPS = ("add", "mul", "gelu", "rmsnorm", "gemv", "scale_bias_relu")
-DTYPES = ("f32", "bf16")
-DTYPE_BYTES = {"f32": 4, "bf16": 2}
+OPS = ("add", "mul", "gelu", "rmsnorm", "gemv", "scale_bias_relu", "quantize", "gemv_f8", "route", "expert_gemv", "expert_sum")
+DTYPES = ("f32", "bf16", "f8_weight", "f8_rows", "routed")
+DTYPE_BYTES = {"f32": 4, "bf16": 2, "f8_weight": 1, "f8_rows": 1, "routed": 8}
 
 
 @dataclass(frozen=True)
@@ -39,15 +39,17 @@ class KernelSpec:
     op: str
     dtype: str
     out: int                      # index of the internal buffer written
-    ins: Tuple[Ref, ...]          # add/mul: (a, b); gelu: (a,); rmsnorm: (x, g); gemv: (W, h); sbr: (x, s, b)
-    n: int                        # output elements (per row for rmsnorm / gemv)
+    ins: Tuple[Ref, ...]          # add/mul: (a, b); gelu: (a,); rmsnorm: (x, g); gemv, gemv_f8: (W, h); sbr: (x, s, b);
+                                  # quantize: (x,); route: (s[, bias]); expert_gemv: (W, h, r); expert_sum: (z, r[, x])
+    n: int                        # output elements (per row for rmsnorm / gemv / gemv_f8, per slot for expert_gemv; route: slots a row)
     segment: int = 0
-    m: int = 0                    # add/mul: broadcast period of b (b[i mod m]); 0 -> n
-    rows: int = 1                 # rmsnorm / gemv batch rows
-    cols: int = 0                 # gemv: input width K; rmsnorm: hidden
-    inner: int = 0                # scale_bias_relu: H*W
+    m: int = 0                    # add/mul: broadcast period of b (b[i mod m]); 0 -> n; route: groups; expert_gemv, expert_sum: slots a row
+    rows: int = 1                 # rmsnorm / gemv / ... batch rows
+    cols: int = 0                 # gemv, gemv_f8, expert_gemv: input width K; rmsnorm, quantize: hidden; route: experts
+    inner: int = 0                # scale_bias_relu: H*W; route: groups kept; expert_gemv: experts
     channels: int = 0             # scale_bias_relu: C
-    eps: float = 0.0              # rmsnorm
+    eps: float = 0.0              # rmsnorm; route: factor of the weights (0: 1)
+    flags: int = 0                # route, expert_gemv
 
 
 @dataclass
