@@ -414,10 +414,299 @@ __global__ __launch_bounds__(kBlock) void k_product(ExpertArgs p) {
     }
 }
 
+// ---- large products -----------------------------------------------------------------------------------------
+// Workgroup b of `total` in an order that gives each of the eight XCDs (workgroups go to them in turn) a stretch of neighbours: they share
+// rows and weights in its L2.
+__device__ __forceinline__ unsigned neighbours(unsigned b, unsigned total) {
+    const unsigned x = b & 7u, each = total >> 3, more = total & 7u;
+    return x * each + (x < more ? x : more) + (b >> 3);
+}
+__device__ const v4u kZeros[1] = {{0u, 0u, 0u, 0u}};
+// 16 bytes a lane from global memory into LDS, lane l's at `to` + 16 l
+__device__ __forceinline__ void direct_to_lds(const unsigned char* base /* uniform */, unsigned off, char* to /* uniform */) {
+    __builtin_amdgcn_global_load_lds((const void PG_GLOBAL*)((const char PG_GLOBAL*)(uintptr_t)base + off), (__attribute__((address_space(3))) void*)to, 16, 0, 0);
+}
+__device__ __forceinline__ void word_to_lds(const unsigned char* base /* uniform */, unsigned off, char* to /* uniform */) {
+    __builtin_amdgcn_global_load_lds((const void PG_GLOBAL*)((const char PG_GLOBAL*)(uintptr_t)base + off), (__attribute__((address_space(3))) void*)to, 4, 0, 0);
+}
+// (the address as it is: some lanes' is not the tensor's)
+__device__ __forceinline__ void direct_to_lds(const unsigned char* from, char* to /* uniform */) {
+    __builtin_amdgcn_global_load_lds((const void PG_GLOBAL*)(uintptr_t)from, (__attribute__((address_space(3))) void*)to, 16, 0, 0);
+}
+// Eight bf16 values from column c of a row of cols >= 8, any alignment, zeros beyond the last: the row's last eight, shifted into place
+__device__ __forceinline__ v4u row8_shifted(const bf16_t* row, int c, int cols) {
+    const int over = c + 8 - cols, s = over < 0 ? 0 : over > 8 ? 8 : over;
+    const int at = c + 8 <= cols ? c : cols - 8;
+    v4u v = *(const v4u_any PG_GLOBAL*)(uintptr_t)(row + at);
+    if (s) {
+        unsigned long long lo = (unsigned long long)v.y << 32 | v.x, hi = (unsigned long long)v.w << 32 | v.z;
+        const int b = 16 * (s & 3);
+        if (s >= 4) { lo = hi; hi = 0; }
+        if (s == 8) lo = 0;
+        if (b) { lo = lo >> b | hi << (64 - b); hi >>= b; }
+        v.x = (unsigned)lo; v.y = (unsigned)(lo >> 32); v.z = (unsigned)hi; v.w = (unsigned)(hi >> 32);
+    }
+    return v;
+}
+
+// The fragments of N tiles of 16 rows, 2 KB apart, of pieces at `a` and at `b`: read and waited for in one piece of assembly (reads of LDS that the
+// compiler places behind loads into LDS wait for all of those first)
+template <int N>
+__device__ __forceinline__ void lds_frags(unsigned a, unsigned b, v4u (&f)[N][2]) {
+    static_assert(N == 1 || N == 2 || N == 4, "tiles");
+    if constexpr (N == 1)
+        asm volatile("ds_read_b128 %0, %2\n\tds_read_b128 %1, %3\n\ts_waitcnt lgkmcnt(0)" : "=&v"(f[0][0]), "=&v"(f[0][1]) : "v"(a), "v"(b) : "memory");
+    else if constexpr (N == 2)
+        asm volatile("ds_read_b128 %0, %4\n\tds_read_b128 %1, %5\n\tds_read_b128 %2, %4 offset:2048\n\tds_read_b128 %3, %5 offset:2048\n\ts_waitcnt lgkmcnt(0)"
+                     : "=&v"(f[0][0]), "=&v"(f[0][1]), "=&v"(f[1][0]), "=&v"(f[1][1]) : "v"(a), "v"(b) : "memory");
+    else
+        asm volatile("ds_read_b128 %0, %8\n\tds_read_b128 %1, %9\n\tds_read_b128 %2, %8 offset:2048\n\tds_read_b128 %3, %9 offset:2048\n\t"
+                     "ds_read_b128 %4, %8 offset:4096\n\tds_read_b128 %5, %9 offset:4096\n\tds_read_b128 %6, %8 offset:6144\n\tds_read_b128 %7, %9 offset:6144\n\t"
+                     "s_waitcnt lgkmcnt(0)"
+                     : "=&v"(f[0][0]), "=&v"(f[0][1]), "=&v"(f[1][0]), "=&v"(f[1][1]), "=&v"(f[2][0]), "=&v"(f[2][1]), "=&v"(f[3][0]), "=&v"(f[3][1])
+                     : "v"(a), "v"(b) : "memory");
+}
+__device__ __forceinline__ unsigned lds_address(const char* p) { return (unsigned)(uintptr_t)(const __attribute__((address_space(3))) char*)p; }
+
+// WR x WJ waves, each RM x JN tiles of 16 rows x 16 outputs, over K in steps of 128 columns (64 where the weights are bf16), two steps in LDS.
+template <Form FORM, bool ROUTED, int RM, int JN, int WR, int WJ>
+__global__ __launch_bounds__(WR * WJ * 64, 2) void k_product_tile(ExpertArgs p) {
+    constexpr bool W8 = FORM != kW16H16, H8 = FORM == kW8H8 || FORM == kW8H8Wide;
+    constexpr int NW = WR * WJ, BM = RM * 16 * WR, BN = JN * 16 * WJ;
+    constexpr int kStep = W8 ? 128 : 64;                      // columns
+    constexpr int HS = W8 && !H8 ? 2 : 1;                     // pieces of 128 bytes that a row of h has of a step
+    constexpr int kHBytes = HS * BM * 128, kStage = kHBytes + BN * 128;
+    constexpr int QH = HS * BM / 8 / NW, QW = BN / 8 / NW;    // loads of eight rows for each wave
+    static_assert(QH * 8 * NW == HS * BM && QW * 8 * NW == BN && (128 % (JN * 16)) == 0, "whole loads; a wave's outputs share their scale");
+    __shared__ __attribute__((aligned(128))) char lds[2 * kStage];
+    __shared__ int slot_of[BM];
+    __shared__ __attribute__((aligned(16))) char lds_exps[2][H8 ? BM * 4 : 16];       // of four steps each
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), l16 = lane & 15, quad = lane >> 4;
+    const int jt = (p.n + BN - 1) / BN;
+    int t, jb;
+    {
+        const unsigned u = neighbours(blockIdx.x, gridDim.x);
+        if (ROUTED) {
+            t = (int)(u / (unsigned)jt);
+            jb = (int)(u % (unsigned)jt);
+        } else {                                             // four tiles of rows, then the next outputs: a stretch is about square
+            const unsigned group = u / (4u * jt), in = u % (4u * jt), first = 4u * group, rows4 = (unsigned)p.tiles - first < 4u ? (unsigned)p.tiles - first : 4u;
+            t = (int)(first + in % rows4);
+            jb = (int)(in / rows4);
+        }
+    }
+    int expert = 0, begin = t * BM, used = p.rows - begin < BM ? p.rows - begin : BM;
+    if constexpr (ROUTED) {
+        if (t >= ((const SortedSlots*)p.sorted)->n_tiles) return;
+        const SortedTile st = sorted_tiles(p.sorted)[t];
+        expert = st.expert;
+        begin = st.begin;
+        used = st.end - st.begin;
+    }
+    for (int i = tid; i < BM; i += NW * 64) {
+        const int at = begin + (i < used ? i : used - 1);
+        slot_of[i] = ROUTED ? sorted_order(p.sorted, p.tiles)[at] : at;
+    }
+    __syncthreads();
+    const int j0 = jb * BN, wr = wave % WR, wj = wave / WR;
+    const int nk = (p.cols + kStep - 1) / kStep, nb = (p.cols + kScaleBlock - 1) / kScaleBlock, nb4 = up_to(nb, 4);
+    const long long kp = (long long)nb * kScaleBlock;
+    f32x4 acc[RM][JN];
+#pragma unroll
+    for (int i = 0; i < RM; i++)
+#pragma unroll
+        for (int j = 0; j < JN; j++) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+    if (!ROUTED || expert >= 0) {
+        const long long wpitch = W8 ? kp : 2ll * p.cols, hpitch = H8 ? kp : 2ll * p.cols;
+        const unsigned char* W = operand<unsigned char>(p.W, p.slots, 0);
+        const unsigned char* h = operand<unsigned char>(p.h, p.slots, 1);
+        const int jblocks = (p.n + kScaleBlock - 1) / kScaleBlock, jblock = (j0 + wj * JN * 16) / kScaleBlock;
+        const float* scales = (const float*)(W + (long long)p.experts * p.n * kp) + ((long long)expert * jblocks + (jblock < jblocks ? jblock : jblocks - 1)) * nb;
+        const int hrows = ROUTED && p.per_slot ? p.rows * p.k : p.rows;
+        // rows as offsets of 32 bits from the first row of the tile, or where rows are gathered from that of the tensor (plan_experts)
+        const long long first = ROUTED ? 0 : begin;
+        auto hrow = [&](int i) { const int s = slot_of[i]; return (unsigned)(ROUTED && !p.per_slot ? s / p.k : ROUTED ? s : s - begin); };
+        W += ((long long)expert * p.n + j0) * wpitch;
+        const unsigned char* hs = h + hrows * kp + first * nb4;
+        h += first * hpitch;
+        // loading: lane l of a load takes the 16-byte piece (l & 7) ^ (l >> 3) of row l >> 3 of its eight, and puts it to place l & 7: fragment
+        // reads of eight neighbouring lanes touch every bank once
+        const int piece = (lane & 7) ^ (lane >> 3);
+        unsigned hp[QH], wp[QW];
+#pragma unroll
+        for (int q = 0; q < QH; q++) hp[q] = hrow(((wave * QH + q) * 8 + (lane >> 3)) % BM) * (unsigned)hpitch + (H8 ? piece * 16 : 0);
+#pragma unroll
+        for (int q = 0; q < QW; q++) {
+            const int j = (wave * QW + q) * 8 + (lane >> 3), last = p.n - 1 - j0;
+            wp[q] = (unsigned)(j < last ? j : last) * (unsigned)wpitch + (W8 ? piece * 16 : 0);
+        }
+        const unsigned exps_at = H8 && wave < BM / 64 ? hrow(wave * 64 + lane) * (unsigned)nb4 : 0u;
+        auto load_exps = [&](int k) {                          // k: a multiple of four
+            if (wave < BM / 64) word_to_lds(hs + k, exps_at, lds_exps[(k >> 2) & 1] + wave * 256);
+        };
+        // (uniform) can 16-byte loads into LDS reach the bf16 rows?
+        const bool direct = (W8 && H8) || (p.cols % 8 == 0 && aligned_to(h, 16) && (W8 || aligned_to(W, 16)));
+        constexpr int kRegs = (H8 ? 0 : QH) + (W8 ? 0 : QW);
+        v4u held[kRegs ? kRegs : 1];
+        auto issue = [&](int k, char* to) {
+#pragma unroll
+            for (int q = 0; q < QH; q++) {
+                const int at = (wave * QH + q) * 8;          // of HS * BM pieces of rows
+                char* const dst = to + at * 128;
+                if constexpr (H8) {
+                    direct_to_lds(h + (long long)k * 128, hp[q], dst);
+                } else {
+                    const int c = k * kStep + (at / BM) * 64 + piece * 8;
+                    if (direct) direct_to_lds(c < p.cols ? h + hp[q] + 2ll * c : (const unsigned char*)kZeros, dst);
+                    else held[q] = row8_shifted((const bf16_t*)(h + hp[q]), c, p.cols);
+                }
+            }
+#pragma unroll
+            for (int q = 0; q < QW; q++) {
+                char* const dst = to + kHBytes + (wave * QW + q) * 1024;
+                if constexpr (W8) {
+                    direct_to_lds(W + (long long)k * 128, wp[q], dst);
+                } else {
+                    const int c = k * kStep + piece * 8;
+                    if (direct) direct_to_lds(c < p.cols ? W + wp[q] + 2ll * c : (const unsigned char*)kZeros, dst);
+                    else held[(H8 ? 0 : QH) + q] = row8_shifted((const bf16_t*)(W + wp[q]), c, p.cols);
+                }
+            }
+        };
+        auto put_held = [&](char* to) {
+            if constexpr (kRegs) {
+                if (!direct) {
+                    if constexpr (!H8)
+#pragma unroll
+                        for (int q = 0; q < QH; q++) *(v4u*)(to + (wave * QH + q) * 1024 + lane * 16) = held[q];
+                    if constexpr (!W8)
+#pragma unroll
+                        for (int q = 0; q < QW; q++) *(v4u*)(to + kHBytes + (wave * QW + q) * 1024 + lane * 16) = held[(H8 ? 0 : QH) + q];
+                }
+            }
+        };
+        // where a lane finds its fragments: row l16 of a tile, pieces quad and quad + 4
+        const int f0 = l16 * 128 + ((quad ^ (l16 & 7)) * 16), f1 = l16 * 128 + (((quad + 4) ^ (l16 & 7)) * 16);
+        // ... and in rows of h in bf16 beside 8-bit weights the columns of those pieces: two pieces in each half of the step
+        const int g0 = HS == 1 ? f0 : l16 * 128 + (((2 * quad) ^ (l16 & 7)) * 16), g1 = HS == 1 ? f1 : l16 * 128 + (((2 * quad + 1) ^ (l16 & 7)) * 16);
+        // lane l: the scale of step l of 64
+        float scale64 = 0.f;
+        auto load_scales = [&](int k) { if (W8) scale64 = *(const float PG_GLOBAL*)(uintptr_t)(scales + (k + lane < nb ? k + lane : nb - 1)); };
+        load_scales(0);
+        if constexpr (H8) load_exps(0);
+        const unsigned lds0 = lds_address(lds);
+        constexpr int kPer = FORM == kW8H8 || FORM == kW16H16 ? 2 : 1;       // tiles of weights that are read at a time
+        issue(0, lds);
+        put_held(lds);
+#pragma unroll 1
+        for (int k = 0; k < nk; k++) {
+            char* const next = lds + ((k + 1) & 1) * kStage;
+            __builtin_amdgcn_s_waitcnt(0x0f70);                // vmcnt(0): this wave's loads of this step
+            __syncthreads();
+            unsigned exps[RM];
+            if constexpr (H8)
+#pragma unroll
+                for (int i = 0; i < RM; i++) exps[i] = (unsigned char)lds_exps[(k >> 2) & 1][((wr * RM + i) * 16 + l16) * 4 + (k & 3)];
+            if (k + 1 < nk) {
+                issue(k + 1, next);
+                if constexpr (H8)
+                    if ((k & 3) == 3) load_exps(k + 1);
+            }
+            const float s = W8 ? __int_as_float(__builtin_amdgcn_readlane(__float_as_int(scale64), k & 63)) : 1.f;
+            if (W8 && (k & 63) == 63) load_scales(k + 1);
+            const unsigned now = lds0 + (unsigned)(k & 1) * kStage;
+            v4u hf[HS][RM][2];
+#pragma unroll
+            for (int q = 0; q < HS; q++) lds_frags<RM>(now + (q * BM + wr * RM * 16) * 128 + g0, now + (q * BM + wr * RM * 16) * 128 + g1, hf[q]);
+#pragma unroll
+            for (int jp = 0; jp < JN; jp += kPer) {
+                v4u wf[kPer][2];
+                const unsigned at = now + kHBytes + (wj * JN + jp) * 16 * 128;
+                lds_frags<kPer>(at + f0, at + f1, wf);
+#pragma unroll
+                for (int jj = 0; jj < kPer; jj++) {
+                    const int j = jp + jj;
+                    if constexpr (FORM == kW8H8) {
+                        const v4u a0 = wf[jj][0], a1 = wf[jj][1];
+                        const v8i A = {(int)a0.x, (int)a0.y, (int)a0.z, (int)a0.w, (int)a1.x, (int)a1.y, (int)a1.z, (int)a1.w};
+#pragma unroll
+                        for (int i = 0; i < RM; i++) {
+                            const v4u b0 = hf[0][i][0], b1 = hf[0][i][1];
+                            const v8i B = {(int)b0.x, (int)b0.y, (int)b0.z, (int)b0.w, (int)b1.x, (int)b1.y, (int)b1.z, (int)b1.w};
+                            const f32x4 sum = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(A, B, f32x4{0.f, 0.f, 0.f, 0.f}, 0, 0, 0, 127, 0, (int)exps[i]);
+#pragma unroll
+                            for (int e = 0; e < 4; e++) acc[i][j][e] = __builtin_fmaf(s, sum[e], acc[i][j][e]);
+                        }
+                    } else if constexpr (FORM == kW16H16) {
+#pragma unroll
+                        for (int i = 0; i < RM; i++)
+#pragma unroll
+                            for (int q = 0; q < 2; q++) acc[i][j] = mfma_bf16(wf[jj][q], hf[0][i][q], acc[i][j]);
+                    } else {
+                        v4u A[4];
+#pragma unroll
+                        for (int q = 0; q < 4; q++) A[q] = half_to_bf16(wf[jj][q >> 1], q & 1);
+#pragma unroll
+                        for (int i = 0; i < RM; i++) {
+                            f32x4 sum = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                            for (int q = 0; q < 4; q++) sum = mfma_bf16(A[q], H8 ? half_to_bf16(hf[0][i][q >> 1], q & 1) : hf[HS == 2 ? q >> 1 : 0][i][q & 1], sum);
+                            const float by = H8 ? __builtin_ldexpf(s, (int)exps[i] - 127) : s;
+#pragma unroll
+                            for (int e = 0; e < 4; e++) acc[i][j][e] = __builtin_fmaf(by, sum[e], acc[i][j][e]);
+                        }
+                    }
+                }
+            }
+            put_held(next);
+        }
+    }
+    const bool four = p.n % 4 == 0;
+#pragma unroll
+    for (int i = 0; i < RM; i++) {
+        const int r = (wr * RM + i) * 16 + l16;
+        if (r >= used) continue;
+        const long long at = (long long)slot_of[r] * p.n;
+#pragma unroll
+        for (int j = 0; j < JN; j++) {
+            const int c = j0 + (wj * JN + j) * 16 + quad * 4;
+            const f32x4 v = acc[i][j];
+            if (p.out_f32) {
+                float* o = (float*)p.out + at + c;
+                if (four && c < p.n) *(f32x4*)o = v;
+                else
+#pragma unroll
+                    for (int e = 0; e < 4; e++) if (c + e < p.n) o[e] = v[e];
+            } else {
+                bf16_t* o = (bf16_t*)p.out + at + c;
+                const unsigned lo = pack2_bf16(v[0], v[1]), hi = pack2_bf16(v[2], v[3]);
+                if (four && c < p.n) *(uint2*)o = uint2{lo, hi};
+                else
+#pragma unroll
+                    for (int e = 0; e < 4; e++) if (c + e < p.n) o[e] = (bf16_t)((e & 2 ? hi : lo) >> (16 * (e & 1)));
+            }
+        }
+    }
+}
+
 template <typename T> const void* route_kernel(int experts) {
     return experts <= 64 ? PG_FN(k_route<T, 1>) : experts <= 128 ? PG_FN(k_route<T, 2>) : experts <= 256 ? PG_FN(k_route<T, 4>) : experts <= 512 ? PG_FN(k_route<T, 8>)
                          : PG_FN(k_route<T, 16>);
 }
+
+struct TileKernel {
+    Form form;
+    const void* plain;
+    const void* routed;
+    int rows, outputs, threads, from;        // from: workgroups
+};
+#define PG_TILE(F, RM, JN, WR, WJ, FROM) {F, PG_FN(k_product_tile<F, false, RM, JN, WR, WJ>), PG_FN(k_product_tile<F, true, RM, JN, WR, WJ>), RM * 16 * WR, JN * 16 * WJ, WR * WJ * 64, FROM}
+const TileKernel kTileKernels[] = {
+    PG_TILE(kW8H8, 4, 8, 4, 2, 128), PG_TILE(kW8H8, 2, 4, 4, 2, 64),
+    PG_TILE(kW8H16, 4, 4, 2, 4, 128), PG_TILE(kW8H16, 2, 4, 4, 2, 64),
+    PG_TILE(kW16H16, 4, 8, 4, 2, 128), PG_TILE(kW16H16, 2, 4, 4, 2, 64),
+    PG_TILE(kW8H8Wide, 4, 4, 2, 4, 128), PG_TILE(kW8H8Wide, 2, 4, 4, 2, 64),
+};
 
 constexpr long long kSmallestTile = 16;
 long long most_tiles(long long slots, long long experts, long long tile) { return slots / tile + std::min(slots, experts + 1); }
@@ -458,17 +747,31 @@ bool plan_experts(int op, int dtype, const Shape& s, Launch* out, Launch* pre) {
     case kGemvF8: case kExpertGemv: {
         const bool routed = op == kExpertGemv, w8 = s.in_dtype[0] == kF8Weight, h8 = s.in_dtype[1] == kF8Rows;
         const long long slots = routed ? s.rows * s.m : s.rows;
-        out->tile = (int)kSmallestTile;
-        const long long tiles = routed ? most_tiles(slots, s.inner, out->tile) : (slots + out->tile - 1) / out->tile;
-        out->tiles = (int)tiles;
-        const long long grid = tiles * ((s.n + 15) / 16);
-        if (grid > 0x7fffffffll) return false;
-        out->arg_bytes = sizeof(ExpertArgs);
-        out->grid = dim3((unsigned)grid);
         const Form form = !w8 ? kW16H16 : !h8 ? kW8H16 : f32 ? kW8H8Wide : kW8H8;
-        out->fn = routed ? (form == kW16H16 ? PG_FN(k_product<kW16H16, true>) : form == kW8H16 ? PG_FN(k_product<kW8H16, true>)
-                            : form == kW8H8 ? PG_FN(k_product<kW8H8, true>) : PG_FN(k_product<kW8H8Wide, true>))
-                         : (form == kW8H16 ? PG_FN(k_product<kW8H16, false>) : form == kW8H8 ? PG_FN(k_product<kW8H8, false>) : PG_FN(k_product<kW8H8Wide, false>));
+        auto with = [&](int tile, int outputs) {
+            out->tile = tile;
+            out->tiles = (int)(routed ? most_tiles(slots, s.inner, tile) : (slots + tile - 1) / tile);
+            const long long grid = out->tiles * ((s.n + outputs - 1) / outputs);
+            out->grid = dim3((unsigned)grid);
+            return grid <= 0x7fffffffll;
+        };
+        out->arg_bytes = sizeof(ExpertArgs);
+        const TileKernel* fit = nullptr;
+        // (their offsets within a tile, and of gathered rows within h, have 32 bits)
+        const long long pitch = w8 ? (s.cols + kScaleBlock - 1) / kScaleBlock * kScaleBlock : 2 * s.cols, hpitch = h8 ? pitch : 2 * s.cols;
+        const bool fits = s.cols >= 8 && 256 * std::max(pitch, hpitch) < (1ll << 32) && (!routed || slots * hpitch < (1ll << 32));
+        for (const TileKernel& k : kTileKernels)
+            if (k.form == form && fits && (!routed || 2 * slots / s.inner >= k.rows) && (slots / (routed ? s.inner : 1) + k.rows - 1) / k.rows * (routed ? s.inner : 1) * ((s.n + k.outputs - 1) / k.outputs) >= k.from) { fit = &k; break; }
+        if (fit) {
+            if (!with(fit->rows, fit->outputs)) return false;
+            out->fn = routed ? fit->routed : fit->plain;
+            out->block = dim3(fit->threads);
+        } else {
+            if (!with((int)kSmallestTile, 16)) return false;
+            out->fn = routed ? (form == kW16H16 ? PG_FN(k_product<kW16H16, true>) : form == kW8H16 ? PG_FN(k_product<kW8H16, true>)
+                                : form == kW8H8 ? PG_FN(k_product<kW8H8, true>) : PG_FN(k_product<kW8H8Wide, true>))
+                             : (form == kW8H16 ? PG_FN(k_product<kW8H16, false>) : form == kW8H8 ? PG_FN(k_product<kW8H8, false>) : PG_FN(k_product<kW8H8Wide, false>));
+        }
         if (routed) {
             pre->fn = PG_FN(k_sort_slots);
             pre->arg_bytes = sizeof(ExpertArgs);
