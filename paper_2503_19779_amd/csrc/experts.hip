@@ -26,72 +26,142 @@ __device__ __forceinline__ float row16_max(float v) {
     return __builtin_fmaxf(v, dpp_take<0x140>(v));
 }
 
+// Eight values from element c of a row on, zeros beyond its last one
+template <typename T>
+__device__ __forceinline__ void eight_of(const T* row, int c, int cols, float* f) {
+    if (c + 8 <= cols) {
+        unsigned w[sizeof(T) * 2];
+#pragma unroll
+        for (int i = 0; i < (int)sizeof(T) / 2; i++) {
+            const v4u v = *(const v4u_any PG_GLOBAL*)(uintptr_t)(row + c + 4 * i);
+            w[4 * i] = v.x; w[4 * i + 1] = v.y; w[4 * i + 2] = v.z; w[4 * i + 3] = v.w;
+        }
+#pragma unroll
+        for (int i = 0; i < 8; i++) f[i] = sizeof(T) == 4 ? __uint_as_float(w[sizeof(T) == 4 ? i : 0]) : __uint_as_float(i & 1 ? w[i / 2] & 0xffff0000u : w[i / 2] << 16);
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; i++) f[i] = c + i < cols ? load_elem(row + c + i) : 0.f;
+    }
+}
+
+// 16 lanes take four neighbouring blocks of a row, whose exponents are one word: four loads (eight for fp32) in flight a lane.
 template <typename T>
 __global__ __launch_bounds__(kBlock) void k_quantize(QuantizeArgs p) {
     const T* x = operand<T>(p.x, p.slots, 0);
-    const int nb = (p.cols + kScaleBlock - 1) / kScaleBlock, nb4 = up_to(nb, 4), lane = threadIdx.x & 15;
-    const long long b = (long long)blockIdx.x * (kBlock / 16) + (threadIdx.x >> 4);
-    const bool live = b < (long long)p.rows * nb;
-    const long long row = live ? b / nb : 0;
-    const int kb = live ? (int)(b - row * nb) : 0, c0 = kb * kScaleBlock + lane * 8;
-    float f[8];
+    const unsigned nb = (unsigned)(p.cols + kScaleBlock - 1) / kScaleBlock, quads = (nb + 3) / 4, lane = threadIdx.x & 15;
+    const unsigned long long total = (unsigned long long)p.rows * quads;
+    const unsigned unit = blockIdx.x * (kBlock / 16) + (threadIdx.x >> 4);          // (fewer than 2^31: plan_experts)
+    const bool live = unit < total;
+    const unsigned row = live ? unit / quads : 0u, quad = live ? unit - row * quads : 0u;
+    const T* from = x + (long long)row * p.cols;
+    float f[4][8];
 #pragma unroll
-    for (int i = 0; i < 8; i++) f[i] = 0.f;
-    const int left = live ? p.cols - c0 : 0;
-    const T* at = x + row * p.cols + c0;
-#pragma unroll
-    for (int i = 0; i < 8; i++) if (i < left) f[i] = load_elem(at + i);
-    float top = 0.f;
-#pragma unroll
-    for (int i = 0; i < 8; i++) {
-        const float a = __builtin_fabsf(f[i]);
-        top = __builtin_fmaxf(top, a < __builtin_inff() ? a : 0.f);
-    }
-    top = row16_max(top);
-    // 448 = 1.75 * 2^8
-    const unsigned u = __float_as_uint(top);
-    int e = (int)(u >> 23) - 127 - 8 + ((u & 0x7fffffu) > 0x600000u ? 1 : 0);
-    e = e < -126 ? -126 : e;
-    const float by = __uint_as_float((unsigned)(127 - e) << 23);
-    unsigned w[2];
-#pragma unroll
-    for (int i = 0; i < 2; i++) {
-        int q = __builtin_amdgcn_cvt_pk_fp8_f32(f[4 * i] * by, f[4 * i + 1] * by, 0, false);
-        q = __builtin_amdgcn_cvt_pk_fp8_f32(f[4 * i + 2] * by, f[4 * i + 3] * by, q, true);
-        w[i] = (unsigned)q;
-    }
-#pragma unroll
-    for (int i = 0; i < 8; i++)
-        if (!(__builtin_fabsf(f[i]) < __builtin_inff())) w[i / 4] = (w[i / 4] & ~(0xffu << (8 * (i & 3)))) | 0x7fu << (8 * (i & 3));
-    if (!live) return;
+    for (int u = 0; u < 4; u++) eight_of(from, (int)(quad * 512 + u * 128 + lane * 8), p.cols, f[u]);
     unsigned char* out = (unsigned char*)p.out;
     const long long kp = (long long)nb * kScaleBlock;
-    uint2 v;
-    v.x = w[0];
-    v.y = w[1];
-    *(uint2*)(out + row * kp + c0) = v;
-    unsigned char* scales = out + (long long)p.rows * kp + row * nb4;
-    if (lane == 0) scales[kb] = (unsigned char)(e + 127);
-    if (kb == nb - 1 && lane >= 1 && nb - 1 + lane < nb4) scales[nb - 1 + lane] = 127;
+    unsigned exps = 0;
+#pragma unroll
+    for (int u = 0; u < 4; u++) {
+        float top = 0.f;
+        bool fine = true;
+#pragma unroll
+        for (int i = 0; i < 8; i++) {
+            const float a = __builtin_fabsf(f[u][i]);
+            const bool is = a < __builtin_inff();
+            fine = fine && is;
+            top = __builtin_fmaxf(top, is ? a : 0.f);
+        }
+        top = row16_max(top);
+        // 448 = 1.75 * 2^8
+        const unsigned bits = __float_as_uint(top);
+        int e = (int)(bits >> 23) - 127 - 8 + ((bits & 0x7fffffu) > 0x600000u ? 1 : 0);
+        e = e < -126 ? -126 : e;
+        const float by = __uint_as_float((unsigned)(127 - e) << 23);
+        unsigned w[2];
+#pragma unroll
+        for (int i = 0; i < 2; i++) {
+            int q = __builtin_amdgcn_cvt_pk_fp8_f32(f[u][4 * i] * by, f[u][4 * i + 1] * by, 0, false);
+            w[i] = (unsigned)__builtin_amdgcn_cvt_pk_fp8_f32(f[u][4 * i + 2] * by, f[u][4 * i + 3] * by, q, true);
+        }
+        if (!fine)
+#pragma unroll
+            for (int i = 0; i < 8; i++)
+                if (!(__builtin_fabsf(f[u][i]) < __builtin_inff())) w[i / 4] = (w[i / 4] & ~(0xffu << (8 * (i & 3)))) | 0x7fu << (8 * (i & 3));
+        const unsigned kb = quad * 4 + u;
+        exps |= (unsigned)(kb < nb ? e + 127 : 127) << (8 * u);
+        if (live && kb < nb) *(uint2*)(out + row * kp + kb * 128 + lane * 8) = uint2{w[0], w[1]};
+    }
+    if (live && lane == 0) *(unsigned*)(out + (long long)p.rows * kp + ((long long)row * quads + quad) * 4) = exps;
 }
 
 // ---- PG_EXPERT_SUM -----------------------------------------------------------------------------------------
+// A lane takes 16 bytes of a row, with up to eight slots' loads in flight.  A row goes to as many lanes as it has such pieces, rounded up to
+// a power of two, or to several workgroups.
+__host__ __device__ inline int sum_lanes(int pieces) {
+    int l = 1;
+    while (l < pieces && l < kBlock) l *= 2;
+    return l;
+}
 template <typename T>
 __global__ __launch_bounds__(kBlock) void k_expert_sum(ExpertSumArgs p) {
+    constexpr int NV = 16 / (int)sizeof(T), kAt = 8;
     const T* z = operand<T>(p.z, p.slots, 0);
     const Routed* r = operand<Routed>(p.r, p.slots, 1);
     const T* x = p.x ? operand<T>(p.x, p.slots, 2) : nullptr;
-    const long long i = (long long)blockIdx.x * kBlock + threadIdx.x;
-    if (i >= (long long)p.rows * p.n) return;
-    const long long row = i / p.n;
-    const int j = (int)(i - row * p.n);
-    float acc = 0.f;
-    for (int t = 0; t < p.k; t++) {
-        const Routed q = r[row * p.k + t];
-        if (q.expert >= 0) acc = __builtin_fmaf(q.weight, load_elem(z + (row * p.k + t) * p.n + j), acc);
+    const int pieces = (p.n + NV - 1) / NV, lanes = sum_lanes(pieces), per_row = (pieces + lanes - 1) / lanes;
+    const unsigned line = blockIdx.x / (unsigned)per_row;
+    const long long row = lanes == kBlock ? (long long)line : (long long)blockIdx.x * (kBlock / lanes) + threadIdx.x / lanes;
+    const int piece = lanes == kBlock ? (int)(blockIdx.x - line * per_row) * kBlock + threadIdx.x : threadIdx.x % lanes;
+    if (row >= p.rows || piece >= pieces) return;
+    const int j = piece * NV, have = p.n - j < NV ? p.n - j : NV;
+    auto fetch = [&](const T* at, unsigned* w) {
+        if (have == NV) {
+            const v4u v = *(const v4u_any PG_GLOBAL*)(uintptr_t)at;
+            w[0] = v.x; w[1] = v.y; w[2] = v.z; w[3] = v.w;
+        } else {
+#pragma unroll
+            for (int i = 0; i < 4; i++) w[i] = 0u;
+#pragma unroll
+            for (int i = 0; i < NV; i++)
+                if (i < have) { if constexpr (sizeof(T) == 4) w[i] = load_raw(at + i); else w[i / 2] |= load_raw(at + i) << (16 * (i & 1)); }
+        }
+    };
+    float acc[NV], f[NV];
+#pragma unroll
+    for (int i = 0; i < NV; i++) acc[i] = 0.f;
+    const Routed* rr = r + row * p.k;
+    const T* zr = z + row * p.k * p.n + j;
+    unsigned wx[4];
+    if (x) fetch(x + row * p.n + j, wx);
+    for (int t0 = 0; t0 < p.k; t0 += kAt) {
+        Routed q[kAt];
+        unsigned w[kAt][4];
+        const int more = p.k - t0;
+#pragma unroll
+        for (int t = 0; t < kAt; t++) q[t] = rr[t0 + (t < more ? t : 0)];
+        // (an empty slot, and what lies behind the last one, is left out of the sum, whatever is fetched in its place)
+#pragma unroll
+        for (int t = 0; t < kAt; t++) if (t < more) fetch(zr + (long long)(t0 + t) * p.n, w[t]);
+#pragma unroll
+        for (int t = 0; t < kAt; t++) {
+            if (t >= more) break;
+            Vec<T, 16>::unpack(w[t], f);
+#pragma unroll
+            for (int i = 0; i < NV; i++) acc[i] = q[t].expert >= 0 ? __builtin_fmaf(q[t].weight, f[i], acc[i]) : acc[i];
+        }
     }
-    if (x) acc += load_elem(x + i);
-    store_elem((T*)p.out + i, acc);
+    if (x) {
+        Vec<T, 16>::unpack(wx, f);
+#pragma unroll
+        for (int i = 0; i < NV; i++) acc[i] += f[i];
+    }
+    T* o = (T*)p.out + row * p.n + j;
+    unsigned w[4];
+    Vec<T, 16>::pack(acc, w);
+    if (have == NV) *(v4u_any*)o = v4u{w[0], w[1], w[2], w[3]};
+    else
+#pragma unroll
+        for (int i = 0; i < NV; i++) if (i < have) store_elem(o + i, acc[i]);
 }
 
 // ---- PG_ROUTE ----------------------------------------------------------------------------------------------
@@ -215,86 +285,89 @@ __global__ __launch_bounds__(kBlock) void k_route(RouteArgs p) {
 }
 
 // ---- PG_EXPERT_GEMV: the slots in the order of their experts ---------------------------------------------------
-constexpr int kSortWaves = 8, kSortMostExperts = 1024;
+constexpr int kSortThreads = 1024, kSortMostExperts = 1024, kSortHeld = 32;
 __device__ __forceinline__ SortedTile* sorted_tiles(void* area) { return (SortedTile*)((SortedSlots*)area + 1); }
 __device__ __forceinline__ int* sorted_order(void* area, int tiles) { return (int*)(sorted_tiles(area) + tiles); }
 
-// One workgroup.  Each wave takes a stretch of the slots, 64 at a time: lanes of one expert find each other by a ballot for each bit of its
-// number.  First how many of each expert a wave has, then from those counts where its first one goes, then the slots to their places:
-// the order is the slots' own, whatever the waves' pace.  Bucket `experts` takes the empty slots.
-__device__ __forceinline__ unsigned long long same_bucket(int id, int bits) {
-    unsigned long long m = ~0ull;
-    for (int b = 0; b < bits; b++) {
-        const unsigned long long on = __ballot((id >> b) & 1);
-        m &= ((id >> b) & 1) ? on : ~on;
-    }
-    return m;
-}
-__global__ __launch_bounds__(kSortWaves * 64) void k_sort_slots(ExpertArgs p) {
-    __shared__ int cnt[kSortWaves][kSortMostExperts + 1];
-    __shared__ int wave_slots[kSortWaves], wave_tiles[kSortWaves];
+// One workgroup: a slot's place among its expert's is what a count in LDS says when it is counted, and from the counts follow the places of the
+// experts.  Slots of an expert come in no fixed order, and a product's rows do not depend on it: each is a row of its own in a tile.  Whole
+// tiles come first, so that the small ones fill what is left of the chip at the end.  Bucket `experts` takes the empty slots.
+__global__ __launch_bounds__(kSortThreads) void k_sort_slots(ExpertArgs p) {
+    __shared__ int cnt[kSortMostExperts + 1];
+    __shared__ int sums[3][kSortThreads / 64];
     const Routed* r = operand<Routed>(p.r, p.slots, 2);
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, buckets = p.experts + 1;
-    const int slots = p.rows * p.k, stretch = (slots + kSortWaves * 64 - 1) / (kSortWaves * 64) * 64;
-    const int s0 = wave * stretch, s1 = s0 + stretch < slots ? s0 + stretch : slots;
-    const int bits = 32 - __builtin_clz(p.experts);
-    for (int i = tid; i < kSortWaves * (kSortMostExperts + 1); i += kSortWaves * 64) (&cnt[0][0])[i] = 0;
-    __syncthreads();
-    auto bucket_of = [&](int s) {
-        const int e = s < s1 ? r[s].expert : 0;
-        return (unsigned)e < (unsigned)p.experts ? e : p.experts;
-    };
-    for (int at = s0; at < s1; at += 64) {
-        const int s = at + lane, id = bucket_of(s);
-        const unsigned long long live = __ballot(s < s1), m = same_bucket(id, bits) & live;
-        if (s < s1 && lane == __builtin_ctzll(m)) cnt[wave][id] += __popcll(m);
+    const int slots = p.rows * p.k;
+    const bool few = slots <= kSortThreads * kSortHeld;      // slots and places stay in registers
+    auto bucket = [&](int e) { return (unsigned)e < (unsigned)p.experts ? e : p.experts; };
+    for (int i = tid; i < buckets; i += kSortThreads) cnt[i] = 0;
+    int id[kSortHeld], place[kSortHeld];
+    if (few) {
+#pragma unroll
+        for (int i = 0; i < kSortHeld; i++) {
+            const int s = i * kSortThreads + tid;
+            id[i] = s < slots ? r[s].expert : -1;
+        }
     }
     __syncthreads();
-    // slots and tiles in front of each bucket: a thread takes three neighbouring buckets (1025 of 512 threads)
-    constexpr int kPer = (kSortMostExperts + 1 + kSortWaves * 64 - 1) / (kSortWaves * 64);
-    int c[kPer], n_slots = 0, n_tiles = 0;
-    for (int q = 0; q < kPer; q++) {
-        const int b = tid * kPer + q;
-        c[q] = 0;
-        if (b < buckets) for (int w = 0; w < kSortWaves; w++) c[q] += cnt[w][b];
-        n_slots += c[q];
-        n_tiles += (c[q] + p.tile - 1) / p.tile;
+    if (few) {
+#pragma unroll
+        for (int i = 0; i < kSortHeld; i++)
+            if (i * kSortThreads + tid < slots) {
+                id[i] = bucket(id[i]);
+                place[i] = atomicAdd(&cnt[id[i]], 1);
+            }
+    } else {
+        for (int s = tid; s < slots; s += kSortThreads) atomicAdd(&cnt[bucket(r[s].expert)], 1);
     }
-    int slots_before = n_slots, tiles_before = n_tiles;
-    for (int d = 1; d < 64; d <<= 1) {
-        const int a = __shfl_up(slots_before, d), b = __shfl_up(tiles_before, d);
-        if (lane >= d) { slots_before += a; tiles_before += b; }
-    }
-    if (lane == 63) { wave_slots[wave] = slots_before; wave_tiles[wave] = tiles_before; }
-    slots_before -= n_slots;
-    tiles_before -= n_tiles;
     __syncthreads();
-    int all = 0;
-    for (int w = 0; w < kSortWaves; w++) {
-        if (w < wave) { slots_before += wave_slots[w]; tiles_before += wave_tiles[w]; }
-        all += wave_tiles[w];
+    // in front of each bucket: slots, whole tiles, others.  A thread takes two neighbouring buckets (1025 of 1024 threads).
+    int c[2], v[3] = {0, 0, 0}, before[3];
+#pragma unroll
+    for (int q = 0; q < 2; q++) {
+        const int b = tid * 2 + q;
+        c[q] = b < buckets ? cnt[b] : 0;
+        v[0] += c[q];
+        v[1] += c[q] / p.tile;
+        v[2] += c[q] % p.tile != 0;
+    }
+#pragma unroll
+    for (int w = 0; w < 3; w++) {
+        before[w] = v[w];
+        for (int d = 1; d < 64; d <<= 1) {
+            const int a = __shfl_up(before[w], d);
+            if (lane >= d) before[w] += a;
+        }
+        if (lane == 63) sums[w][wave] = before[w];
+        before[w] -= v[w];
+    }
+    __syncthreads();
+    int whole = 0, all = 0;
+    for (int u = 0; u < kSortThreads / 64; u++) {
+        if (u < wave) for (int w = 0; w < 3; w++) before[w] += sums[w][u];
+        whole += sums[1][u];
+        all += sums[1][u] + sums[2][u];
     }
     SortedTile* tiles = sorted_tiles(p.sorted);
-    for (int q = 0; q < kPer; q++) {
-        const int b = tid * kPer + q;
+#pragma unroll
+    for (int q = 0; q < 2; q++) {
+        const int b = tid * 2 + q;
         if (b >= buckets) break;
-        for (int i = 0; i < c[q]; i += p.tile)
-            tiles[tiles_before++] = SortedTile{b < p.experts ? b : -1, slots_before + i, slots_before + (i + p.tile < c[q] ? i + p.tile : c[q]), 0};
-        int base = slots_before;
-        for (int w = 0; w < kSortWaves; w++) { const int n = cnt[w][b]; cnt[w][b] = base; base += n; }
-        slots_before += c[q];
+        const int first = before[0], expert = b < p.experts ? b : -1, n = c[q] / p.tile;
+        for (int i = 0; i < n; i++) tiles[before[1]++] = SortedTile{expert, first + i * p.tile, first + (i + 1) * p.tile, 0};
+        if (c[q] % p.tile) tiles[whole + before[2]++] = SortedTile{expert, first + n * p.tile, first + c[q], 0};
+        cnt[b] = first;
+        before[0] += c[q];
     }
     if (tid == 0) ((SortedSlots*)p.sorted)->n_tiles = all;
     __syncthreads();
     int* order = sorted_order(p.sorted, p.tiles);
-    for (int at = s0; at < s1; at += 64) {
-        const int s = at + lane, id = bucket_of(s);
-        const unsigned long long live = __ballot(s < s1), m = same_bucket(id, bits) & live;
-        if (s < s1) {
-            const int base = cnt[wave][id];
-            order[base + __popcll(m & ((1ull << lane) - 1ull))] = s;
-            if (lane == __builtin_ctzll(m)) cnt[wave][id] = base + __popcll(m);
-        }
+    if (few) {
+#pragma unroll
+        for (int i = 0; i < kSortHeld; i++)
+            if (i * kSortThreads + tid < slots) order[cnt[id[i]] + place[i]] = i * kSortThreads + tid;
+    } else {
+        for (int s = tid; s < slots; s += kSortThreads) order[atomicAdd(&cnt[bucket(r[s].expert)], 1)] = s;
     }
 }
 
@@ -485,11 +558,12 @@ __global__ __launch_bounds__(WR * WJ * 64, 2) void k_product_tile(ExpertArgs p) 
     const int jt = (p.n + BN - 1) / BN;
     int t, jb;
     {
-        const unsigned u = neighbours(blockIdx.x, gridDim.x);
-        if (ROUTED) {
-            t = (int)(u / (unsigned)jt);
-            jb = (int)(u % (unsigned)jt);
+        if (ROUTED) {                                        // each XCD takes two tiles in turn, which mostly are one expert's, with all their outputs
+            const unsigned in = (blockIdx.x >> 3) % (2u * jt);
+            t = (int)((blockIdx.x >> 3) / (2u * jt) * 16 + (blockIdx.x & 7u) * 2 + (in & 1u));
+            jb = (int)(in >> 1);
         } else {                                             // four tiles of rows, then the next outputs: a stretch is about square
+            const unsigned u = neighbours(blockIdx.x, gridDim.x);
             const unsigned group = u / (4u * jt), in = u % (4u * jt), first = 4u * group, rows4 = (unsigned)p.tiles - first < 4u ? (unsigned)p.tiles - first : 4u;
             t = (int)(first + in % rows4);
             jb = (int)(in / rows4);
@@ -508,7 +582,7 @@ __global__ __launch_bounds__(WR * WJ * 64, 2) void k_product_tile(ExpertArgs p) 
         slot_of[i] = ROUTED ? sorted_order(p.sorted, p.tiles)[at] : at;
     }
     __syncthreads();
-    const int j0 = jb * BN, wr = wave % WR, wj = wave / WR;
+    const int j0 = jb * BN, wr = wave / WJ, wj = wave % WJ;      // (waves w and w + 4 share a SIMD: other rows, of which a small tile may have none)
     const int nk = (p.cols + kStep - 1) / kStep, nb = (p.cols + kScaleBlock - 1) / kScaleBlock, nb4 = up_to(nb, 4);
     const long long kp = (long long)nb * kScaleBlock;
     f32x4 acc[RM][JN];
@@ -615,6 +689,7 @@ __global__ __launch_bounds__(WR * WJ * 64, 2) void k_product_tile(ExpertArgs p) 
             const float s = W8 ? __int_as_float(__builtin_amdgcn_readlane(__float_as_int(scale64), k & 63)) : 1.f;
             if (W8 && (k & 63) == 63) load_scales(k + 1);
             const unsigned now = lds0 + (unsigned)(k & 1) * kStage;
+            if (wr * RM * 16 < used) {
             v4u hf[HS][RM][2];
 #pragma unroll
             for (int q = 0; q < HS; q++) lds_frags<RM>(now + (q * BM + wr * RM * 16) * 128 + g0, now + (q * BM + wr * RM * 16) * 128 + g1, hf[q]);
@@ -657,6 +732,7 @@ __global__ __launch_bounds__(WR * WJ * 64, 2) void k_product_tile(ExpertArgs p) 
                         }
                     }
                 }
+            }
             }
             put_held(next);
         }
@@ -726,11 +802,11 @@ bool plan_experts(int op, int dtype, const Shape& s, Launch* out, Launch* pre) {
     const bool f32 = dtype == kF32;
     switch (op) {
     case kQuantize: {
-        const long long blocks = s.rows * ((s.cols + kScaleBlock - 1) / kScaleBlock);
-        if (blocks > (1ll << 34)) return false;
+        const long long units = s.rows * (((s.cols + kScaleBlock - 1) / kScaleBlock + 3) / 4);
+        if (units >= (1ll << 31)) return false;
         out->fn = f32 ? PG_FN(k_quantize<float>) : PG_FN(k_quantize<bf16_t>);
         out->arg_bytes = sizeof(QuantizeArgs);
-        out->grid = dim3(blocks_for(blocks, kBlock / 16));
+        out->grid = dim3(blocks_for(units, kBlock / 16));
         return true;
     }
     case kRoute:
@@ -738,12 +814,15 @@ bool plan_experts(int op, int dtype, const Shape& s, Launch* out, Launch* pre) {
         out->arg_bytes = sizeof(RouteArgs);
         out->grid = dim3(blocks_for(s.rows, kBlock / 64));
         return true;
-    case kExpertSum:
-        if (s.rows * s.n > (1ll << 38)) return false;
+    case kExpertSum: {
+        const int pieces = (int)((s.n + (f32 ? 4 : 8) - 1) / (f32 ? 4 : 8)), lanes = sum_lanes(pieces);
+        const long long grid = lanes == kBlock ? s.rows * blocks_for(pieces, kBlock) : (s.rows + kBlock / lanes - 1) / (kBlock / lanes);
+        if (grid > 0x7fffffffll) return false;
         out->fn = f32 ? PG_FN(k_expert_sum<float>) : PG_FN(k_expert_sum<bf16_t>);
         out->arg_bytes = sizeof(ExpertSumArgs);
-        out->grid = dim3(blocks_for(s.rows * s.n, kBlock));
+        out->grid = dim3((unsigned)grid);
         return true;
+    }
     case kGemvF8: case kExpertGemv: {
         const bool routed = op == kExpertGemv, w8 = s.in_dtype[0] == kF8Weight, h8 = s.in_dtype[1] == kF8Rows;
         const long long slots = routed ? s.rows * s.m : s.rows;
@@ -751,7 +830,7 @@ bool plan_experts(int op, int dtype, const Shape& s, Launch* out, Launch* pre) {
         auto with = [&](int tile, int outputs) {
             out->tile = tile;
             out->tiles = (int)(routed ? most_tiles(slots, s.inner, tile) : (slots + tile - 1) / tile);
-            const long long grid = out->tiles * ((s.n + outputs - 1) / outputs);
+            const long long grid = (routed && tile > kSmallestTile ? (out->tiles + 15) / 16 * 16 : out->tiles) * ((s.n + outputs - 1) / outputs);
             out->grid = dim3((unsigned)grid);
             return grid <= 0x7fffffffll;
         };
@@ -775,7 +854,7 @@ bool plan_experts(int op, int dtype, const Shape& s, Launch* out, Launch* pre) {
         if (routed) {
             pre->fn = PG_FN(k_sort_slots);
             pre->arg_bytes = sizeof(ExpertArgs);
-            pre->block = dim3(kSortWaves * 64);
+            pre->block = dim3(kSortThreads);
         }
         return true;
     }
