@@ -3,6 +3,7 @@
 #include "device.h"
 
 #include <algorithm>
+#include <type_traits>
 
 namespace pgk {
 namespace {
@@ -295,6 +296,7 @@ __device__ __forceinline__ int* sorted_order(void* area, int tiles) { return (in
 __global__ __launch_bounds__(kSortThreads) void k_sort_slots(ExpertArgs p) {
     __shared__ int cnt[kSortMostExperts + 1];
     __shared__ int sums[3][kSortThreads / 64];
+    __shared__ int ordered[kSortThreads * kSortHeld];
     const Routed* r = operand<Routed>(p.r, p.slots, 2);
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, buckets = p.experts + 1;
     const int slots = p.rows * p.k;
@@ -362,10 +364,12 @@ __global__ __launch_bounds__(kSortThreads) void k_sort_slots(ExpertArgs p) {
     if (tid == 0) ((SortedSlots*)p.sorted)->n_tiles = all;
     __syncthreads();
     int* order = sorted_order(p.sorted, p.tiles);
-    if (few) {
+    if (few) {                       // (by way of LDS: 64 scattered stores of a wave take 64 lines' time)
 #pragma unroll
         for (int i = 0; i < kSortHeld; i++)
-            if (i * kSortThreads + tid < slots) order[cnt[id[i]] + place[i]] = i * kSortThreads + tid;
+            if (i * kSortThreads + tid < slots) ordered[cnt[id[i]] + place[i]] = i * kSortThreads + tid;
+        __syncthreads();
+        for (int s = tid; s < slots; s += kSortThreads) order[s] = ordered[s];
     } else {
         for (int s = tid; s < slots; s += kSortThreads) order[atomicAdd(&cnt[bucket(r[s].expert)], 1)] = s;
     }
@@ -737,32 +741,43 @@ __global__ __launch_bounds__(WR * WJ * 64, 2) void k_product_tile(ExpertArgs p) 
             put_held(next);
         }
     }
-    const bool four = p.n % 4 == 0;
+    // Out by whole pieces of rows: 16 rows of a wave at a time go through its own part of LDS (16 bytes between rows: other banks), 16 bytes a lane from there.
+    __builtin_amdgcn_s_waitcnt(0x0f70);
+    __syncthreads();                                           // the last step has been read
+    auto emit = [&](auto* out) {
+        using O = std::remove_pointer_t<decltype(out)>;
+        constexpr int NV = 16 / (int)sizeof(O), kPitch = JN * 16 * (int)sizeof(O) + 16, kLanes = JN * 16 / NV, kRowsAt = 64 / kLanes;
+        static_assert(NW * 16 * kPitch <= 2 * kStage, "the waves' parts");
+        char* const mine = lds + wave * 16 * kPitch;
+        const int c = j0 + wj * JN * 16 + lane % kLanes * NV;
 #pragma unroll
-    for (int i = 0; i < RM; i++) {
-        const int r = (wr * RM + i) * 16 + l16;
-        if (r >= used) continue;
-        const long long at = (long long)slot_of[r] * p.n;
+        for (int i = 0; i < RM; i++) {
+            if ((wr * RM + i) * 16 >= used) break;
 #pragma unroll
-        for (int j = 0; j < JN; j++) {
-            const int c = j0 + (wj * JN + j) * 16 + quad * 4;
-            const f32x4 v = acc[i][j];
-            if (p.out_f32) {
-                float* o = (float*)p.out + at + c;
-                if (four && c < p.n) *(f32x4*)o = v;
-                else
-#pragma unroll
-                    for (int e = 0; e < 4; e++) if (c + e < p.n) o[e] = v[e];
-            } else {
-                bf16_t* o = (bf16_t*)p.out + at + c;
-                const unsigned lo = pack2_bf16(v[0], v[1]), hi = pack2_bf16(v[2], v[3]);
-                if (four && c < p.n) *(uint2*)o = uint2{lo, hi};
-                else
-#pragma unroll
-                    for (int e = 0; e < 4; e++) if (c + e < p.n) o[e] = (bf16_t)((e & 2 ? hi : lo) >> (16 * (e & 1)));
+            for (int j = 0; j < JN; j++) {
+                char* const at = mine + l16 * kPitch + (j * 16 + quad * 4) * (int)sizeof(O);
+                const f32x4 v = acc[i][j];
+                if constexpr (sizeof(O) == 4) *(f32x4*)at = v;
+                else *(uint2*)at = uint2{pack2_bf16(v[0], v[1]), pack2_bf16(v[2], v[3])};
             }
+            __builtin_amdgcn_wave_barrier();
+#pragma unroll
+            for (int q = 0; q < 16 / kRowsAt; q++) {
+                const int r = q * kRowsAt + lane / kLanes, row = (wr * RM + i) * 16 + r;
+                const v4u v = *(const v4u*)(mine + r * kPitch + lane % kLanes * 16);
+                if (row >= used || c >= p.n) continue;
+                O* o = out + (long long)slot_of[row] * p.n + c;
+                if (c + NV <= p.n) *(v4u_any PG_GLOBAL*)(uintptr_t)o = v;
+                else
+#pragma unroll
+                    for (int e = 0; e < NV; e++)
+                        if (c + e < p.n) o[e] = (O)(sizeof(O) == 4 ? v[e & 3] : v[(e / 2) & 3] >> (16 * (e & 1)));
+            }
+            __builtin_amdgcn_wave_barrier();
         }
-    }
+    };
+    if (p.out_f32) emit((unsigned*)p.out);
+    else emit((bf16_t*)p.out);
 }
 
 template <typename T> const void* route_kernel(int experts) {
