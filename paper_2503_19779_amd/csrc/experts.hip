@@ -3,6 +3,7 @@
 #include "device.h"
 
 #include <algorithm>
+#include <iterator>
 #include <type_traits>
 
 namespace pgk {
@@ -376,20 +377,26 @@ __global__ __launch_bounds__(kSortThreads) void k_sort_slots(ExpertArgs p) {
 }
 
 // ---- products ----------------------------------------------------------------------------------------------
-// Eight bf16 values of a row from column c on, zeros beyond its last one
-__device__ __forceinline__ v4u row8(const bf16_t* row, int c, int cols) {
-    v4u v = {0u, 0u, 0u, 0u};
-    if (c + 8 <= cols) {
-        v = *(const v4u_any PG_GLOBAL*)(uintptr_t)(row + c);
-    } else {
-        unsigned w[4] = {0u, 0u, 0u, 0u};
-#pragma unroll
-        for (int i = 0; i < 8; i++) if (c + i < cols) w[i / 2] |= (unsigned)row[c + i] << (16 * (i & 1));
-        v.x = w[0]; v.y = w[1]; v.z = w[2]; v.w = w[3];
-    }
+// Eight bf16 values from column c of a row of cols >= 8 on, at any element boundary, zeros beyond its last one: what 16 bytes load from inside the row, and the
+// shift that puts it in place
+__device__ __forceinline__ v4u row8_raw(const bf16_t* row, int c, int cols) {
+    return *(const v4u_any PG_GLOBAL*)(uintptr_t)(row + (c + 8 <= cols ? c : cols - 8));
+}
+__device__ __forceinline__ v4u row8_fix(v4u v, int c, int cols) {
+    const int over = c + 8 - cols, s = over < 0 ? 0 : over > 8 ? 8 : over, b = 16 * (s & 3);
+    unsigned long long lo = (unsigned long long)v.y << 32 | v.x, hi = (unsigned long long)v.w << 32 | v.z;
+    if (s >= 4) { lo = s == 8 ? 0 : hi; hi = 0; }
+    if (b) { lo = lo >> b | hi << (64 - b); hi >>= b; }
+    v.x = (unsigned)lo; v.y = (unsigned)(lo >> 32); v.z = (unsigned)hi; v.w = (unsigned)(hi >> 32);
     return v;
 }
-__device__ __forceinline__ v4u bytes16(const unsigned char* p) { return *(const v4u PG_GLOBAL*)(uintptr_t)p; }
+// ... of a row of any length, one by one
+__device__ __forceinline__ v4u row8_short(const bf16_t* row, int c, int cols) {
+    unsigned w[4] = {0u, 0u, 0u, 0u};
+#pragma unroll
+    for (int i = 0; i < 8; i++) if (c + i < cols) w[i / 2] |= (unsigned)row[c + i] << (16 * (i & 1));
+    return v4u{w[0], w[1], w[2], w[3]};
+}
 template <bool HI> __device__ __forceinline__ unsigned f8_to_bf16(unsigned w) {
     return __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, 1.0f, HI));
 }
@@ -410,94 +417,50 @@ __device__ __forceinline__ f32x4 mfma_bf16(v4u a, v4u b, f32x4 c) {
 // show.  An fp32 output would, so there both operands become bf16, exactly, and the bf16 instruction, which sums in fp32, takes them.
 enum Form : int { kW16H16, kW8H16, kW8H8, kW8H8Wide };
 
-// A workgroup: 16 outputs of up to 16 rows of h; its four waves take the blocks of 128 columns in turn.
-template <Form FORM, bool ROUTED>
-__global__ __launch_bounds__(kBlock) void k_product(ExpertArgs p) {
-    constexpr bool W8 = FORM != kW16H16, H8 = FORM == kW8H8 || FORM == kW8H8Wide;
-    __shared__ float part[4][16][17];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, l16 = lane & 15, quad = lane >> 4;
-    const int jt = (p.n + 15) / 16;
-    const int t = (int)(blockIdx.x / (unsigned)jt), j0 = (int)(blockIdx.x % (unsigned)jt) * 16;
-    int expert = 0, begin = t * 16, end = begin + 16 < p.rows ? begin + 16 : p.rows;
-    const int* order = nullptr;
-    if constexpr (ROUTED) {
-        if (t >= ((const SortedSlots*)p.sorted)->n_tiles) return;
+// The tile of slots that a workgroup of a routed product takes: its expert and how many slots.  From the sorted slots, or, up to kFewSlots of them,
+// worked out by each wave for itself (a dispatch in front costs more): slot i, in lane i, is the rank-th of its expert; the slots whose rank is a
+// multiple of the tile open a tile each, and those are numbered in the order of the slots.  expert -2: there is no tile t.
+constexpr int kFewSlots = 64;
+struct TileOf { int expert, used; int begin; unsigned long long members; };
+template <int TILE>
+__device__ __forceinline__ TileOf routed_tile(const ExpertArgs& p, int t) {
+    if (p.sorted) {
+        if (t >= ((const SortedSlots*)p.sorted)->n_tiles) return TileOf{-2, 0, 0, 0};
         const SortedTile st = sorted_tiles(p.sorted)[t];
-        expert = st.expert;
-        begin = st.begin;
-        end = st.end;
-        order = sorted_order(p.sorted, p.tiles);
+        return TileOf{st.expert, st.end - st.begin, st.begin, 0};
     }
-    auto slot_of = [&](int i) { return ROUTED ? order[begin + i] : begin + i; };      // the i-th slot of the tile
-    const int used = end - begin;
-    f32x4 acc = {0.f, 0.f, 0.f, 0.f};
-    const int nb = (p.cols + kScaleBlock - 1) / kScaleBlock;
-    const long long kp = (long long)nb * kScaleBlock;
-    if (!ROUTED || expert >= 0) {
-        const int j = j0 + l16 < p.n ? j0 + l16 : p.n - 1;
-        const int slot = slot_of(l16 < used ? l16 : used - 1);
-        const long long hrow = ROUTED && !p.per_slot ? slot / p.k : slot;
-        const int hrows = ROUTED && p.per_slot ? p.rows * p.k : p.rows;
-        const unsigned char* w8 = operand<unsigned char>(p.W, p.slots, 0);
-        const float* scales = (const float*)(w8 + (long long)p.experts * p.n * kp) + ((long long)expert * ((p.n + kScaleBlock - 1) / kScaleBlock) + j0 / kScaleBlock) * nb;
-        const bf16_t* w16 = (const bf16_t*)w8 + ((long long)expert * p.n + j) * p.cols;
-        w8 += ((long long)expert * p.n + j) * kp;
-        const unsigned char* h8 = operand<unsigned char>(p.h, p.slots, 1);
-        const bf16_t* h16 = (const bf16_t*)h8 + hrow * p.cols;
-        const unsigned char* hs = h8 + hrows * kp + hrow * up_to(nb, 4);
-        h8 += hrow * kp;
-        for (int kb = wave; kb < nb; kb += 4) {
-            // a lane's 32 of the block's 128 columns: 16 at quad * 16 and 16 at 64 + quad * 16
-            f32x4 sum = {0.f, 0.f, 0.f, 0.f};
-            const int c0 = kb * kScaleBlock + quad * 16;
-            v4u a[2];
-            if constexpr (W8) {
-                a[0] = bytes16(w8 + c0);
-                a[1] = bytes16(w8 + c0 + 64);
-            }
-            v4u b[2];
-            if constexpr (FORM == kW8H8Wide) {
-                b[0] = bytes16(h8 + c0);
-                b[1] = bytes16(h8 + c0 + 64);
-            }
-            if constexpr (FORM == kW8H8) {
-                const v4u b0 = bytes16(h8 + c0), b1 = bytes16(h8 + c0 + 64);
-                const v8i A = {(int)a[0].x, (int)a[0].y, (int)a[0].z, (int)a[0].w, (int)a[1].x, (int)a[1].y, (int)a[1].z, (int)a[1].w};
-                const v8i B = {(int)b0.x, (int)b0.y, (int)b0.z, (int)b0.w, (int)b1.x, (int)b1.y, (int)b1.z, (int)b1.w};
-                sum = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(A, B, sum, 0, 0, 0, 127, 0, (int)hs[kb]);
-            } else {
-#pragma unroll
-                for (int q = 0; q < 4; q++) {
-                    const int c = c0 + (q >> 1) * 64 + (q & 1) * 8;
-                    const v4u A = W8 ? half_to_bf16(a[q >> 1], q & 1) : row8(w16, c, p.cols);
-                    sum = mfma_bf16(A, H8 ? half_to_bf16(b[q >> 1], q & 1) : row8(h16, c, p.cols), sum);
-                }
-            }
-            float s = W8 ? scales[kb] : 1.f;
-            if constexpr (FORM == kW8H8Wide) s = __builtin_ldexpf(s, (int)hs[kb] - 127);
-#pragma unroll
-            for (int i = 0; i < 4; i++) acc[i] = W8 ? __builtin_fmaf(s, sum[i], acc[i]) : acc[i] + sum[i];
-        }
+    const Routed* r = operand<Routed>(p.r, p.slots, 2);
+    const int slots = p.rows * p.k, lane = threadIdx.x & 63;
+    const int e = lane < slots ? r[lane].expert : 0, id = (unsigned)e < (unsigned)p.experts ? e : p.experts;
+    unsigned long long same = slots < 64 ? (1ull << slots) - 1ull : ~0ull;
+    const unsigned long long all = same, before = (1ull << lane) - 1ull;
+    for (int b = 0; b < 32 - __builtin_clz(p.experts); b++) {
+        const unsigned long long on = __ballot((id >> b) & 1);
+        same &= ((id >> b) & 1) ? on : ~on;
     }
-#pragma unroll
-    for (int i = 0; i < 4; i++) part[wave][l16][quad * 4 + i] = acc[i];
-    __syncthreads();
-    const int m = threadIdx.x >> 4, c = threadIdx.x & 15;
-    if (m < used && j0 + c < p.n) {
-        const float y = (part[0][m][c] + part[1][m][c]) + (part[2][m][c] + part[3][m][c]);
-        const long long at = (long long)slot_of(m) * p.n + j0 + c;
-        if (p.out_f32) ((float*)p.out)[at] = y;
-        else ((bf16_t*)p.out)[at] = (bf16_t)f32_to_bf16(y);
+    const int rank = __popcll(same & before);
+    const unsigned long long opens = __ballot(rank % TILE == 0) & all;
+    const unsigned long long mine = __ballot((int)__popcll(opens & before) == t) & opens;
+    if (!mine) return TileOf{-2, 0, 0, 0};
+    const int at = __builtin_ctzll(mine), expert = __builtin_amdgcn_readlane(id, at), first = __builtin_amdgcn_readlane(rank, at);
+    const unsigned long long members = __ballot(id == expert && rank >= first && rank < first + TILE) & all;
+    return TileOf{expert < p.experts ? expert : -1, (int)__popcll(members), 0, members};
+}
+// Its slots to `list`, the last one again where there are fewer than TILE: by each wave for itself, all the same
+template <int TILE>
+__device__ __forceinline__ void tile_slots(const ExpertArgs& p, const TileOf& tile, int* list) {
+    const int lane = threadIdx.x & 63;
+    if (p.sorted) {
+        const int* order = sorted_order(p.sorted, p.tiles) + tile.begin;
+        for (int i = lane; i < TILE; i += 64) list[i] = order[i < tile.used ? i : tile.used - 1];
+    } else {
+        const int place = __popcll(tile.members & ((1ull << lane) - 1ull)), last = 63 - __builtin_clzll(tile.members);
+        if ((tile.members >> lane) & 1ull) list[place] = lane;
+        for (int i = lane; i < TILE; i += 64) if (i >= tile.used) list[i] = last;
     }
+    __builtin_amdgcn_wave_barrier();
 }
 
-// ---- large products -----------------------------------------------------------------------------------------
-// Workgroup b of `total` in an order that gives each of the eight XCDs (workgroups go to them in turn) a stretch of neighbours: they share
-// rows and weights in its L2.
-__device__ __forceinline__ unsigned neighbours(unsigned b, unsigned total) {
-    const unsigned x = b & 7u, each = total >> 3, more = total & 7u;
-    return x * each + (x < more ? x : more) + (b >> 3);
-}
 __device__ const v4u kZeros[1] = {{0u, 0u, 0u, 0u}};
 // 16 bytes a lane from global memory into LDS, lane l's at `to` + 16 l
 __device__ __forceinline__ void direct_to_lds(const unsigned char* base /* uniform */, unsigned off, char* to /* uniform */) {
@@ -506,26 +469,17 @@ __device__ __forceinline__ void direct_to_lds(const unsigned char* base /* unifo
 __device__ __forceinline__ void word_to_lds(const unsigned char* base /* uniform */, unsigned off, char* to /* uniform */) {
     __builtin_amdgcn_global_load_lds((const void PG_GLOBAL*)((const char PG_GLOBAL*)(uintptr_t)base + off), (__attribute__((address_space(3))) void*)to, 4, 0, 0);
 }
+__device__ __forceinline__ void word_to_lds(const unsigned char* from, char* to /* uniform */) {
+    __builtin_amdgcn_global_load_lds((const void PG_GLOBAL*)(uintptr_t)from, (__attribute__((address_space(3))) void*)to, 4, 0, 0);
+}
 // (the address as it is: some lanes' is not the tensor's)
 __device__ __forceinline__ void direct_to_lds(const unsigned char* from, char* to /* uniform */) {
     __builtin_amdgcn_global_load_lds((const void PG_GLOBAL*)(uintptr_t)from, (__attribute__((address_space(3))) void*)to, 16, 0, 0);
 }
-// Eight bf16 values from column c of a row of cols >= 8, any alignment, zeros beyond the last: the row's last eight, shifted into place
 __device__ __forceinline__ v4u row8_shifted(const bf16_t* row, int c, int cols) {
-    const int over = c + 8 - cols, s = over < 0 ? 0 : over > 8 ? 8 : over;
-    const int at = c + 8 <= cols ? c : cols - 8;
-    v4u v = *(const v4u_any PG_GLOBAL*)(uintptr_t)(row + at);
-    if (s) {
-        unsigned long long lo = (unsigned long long)v.y << 32 | v.x, hi = (unsigned long long)v.w << 32 | v.z;
-        const int b = 16 * (s & 3);
-        if (s >= 4) { lo = hi; hi = 0; }
-        if (s == 8) lo = 0;
-        if (b) { lo = lo >> b | hi << (64 - b); hi >>= b; }
-        v.x = (unsigned)lo; v.y = (unsigned)(lo >> 32); v.z = (unsigned)hi; v.w = (unsigned)(hi >> 32);
-    }
-    return v;
+    const v4u v = row8_raw(row, c, cols);
+    return c + 8 <= cols ? v : row8_fix(v, c, cols);
 }
-
 // The fragments of N tiles of 16 rows, 2 KB apart, of pieces at `a` and at `b`: read and waited for in one piece of assembly (reads of LDS that the
 // compiler places behind loads into LDS wait for all of those first)
 template <int N>
@@ -545,8 +499,209 @@ __device__ __forceinline__ void lds_frags(unsigned a, unsigned b, v4u (&f)[N][2]
 }
 __device__ __forceinline__ unsigned lds_address(const char* p) { return (unsigned)(uintptr_t)(const __attribute__((address_space(3))) char*)p; }
 
-// WR x WJ waves, each RM x JN tiles of 16 rows x 16 outputs, over K in steps of 128 columns (64 where the weights are bf16), two steps in LDS.
-template <Form FORM, bool ROUTED, int RM, int JN, int WR, int WJ>
+// N bytes, 64 bytes apart
+template <int N>
+__device__ __forceinline__ void lds_bytes(unsigned at, unsigned (&v)[N]) {
+    static_assert(N == 1 || N == 2 || N == 4, "tiles");
+    if constexpr (N == 1) asm volatile("ds_read_u8 %0, %1\n\ts_waitcnt lgkmcnt(0)" : "=&v"(v[0]) : "v"(at) : "memory");
+    else if constexpr (N == 2)
+        asm volatile("ds_read_u8 %0, %2\n\tds_read_u8 %1, %2 offset:64\n\ts_waitcnt lgkmcnt(0)" : "=&v"(v[0]), "=&v"(v[1]) : "v"(at) : "memory");
+    else
+        asm volatile("ds_read_u8 %0, %4\n\tds_read_u8 %1, %4 offset:64\n\tds_read_u8 %2, %4 offset:128\n\tds_read_u8 %3, %4 offset:192\n\ts_waitcnt lgkmcnt(0)"
+                     : "=&v"(v[0]), "=&v"(v[1]), "=&v"(v[2]), "=&v"(v[3]) : "v"(at) : "memory");
+}
+template <int N> __device__ __forceinline__ void wait_loads() { asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory"); }
+
+// Products with few rows for an expert, where what bounds it is the way of the weights: a workgroup takes 16 * JT outputs of up to 16 * MT rows of h, its NW
+// waves the steps of K in turn (128 columns; 64 where the weights are bf16), each through a ring of S steps in its own part of LDS, with no barrier
+// until the partial sums meet.  Loads go by whole lines of eight rows, straight into LDS: as fragments in registers, neighbouring lanes took
+// 16 bytes of a row each, and a load the time of 64 lines (64 rows of 4096 columns 16 us for any number of outputs).
+template <Form FORM, bool ROUTED, int MT, int JT, int S, int NW>
+__global__ __launch_bounds__(NW * 64, (S * NW * ((FORM == kW8H16 ? 2 : 1) * MT + JT) * 2048 <= 76 * 1024 ? 2 : 1) * NW / 4) void k_product(ExpertArgs p) {
+    constexpr bool W8 = FORM != kW16H16, H8 = FORM == kW8H8 || FORM == kW8H8Wide;
+    constexpr int TILE = 16 * MT, OUTS = 16 * JT, kStep = W8 ? 128 : 64;
+    constexpr int HS = W8 && !H8 ? 2 : 1;                     // pieces of 128 bytes that a row of h has of a step
+    constexpr int QH = HS * MT * 2, QW = JT * 2, kLoads = QH + QW + (H8 ? 1 : 0);
+    constexpr int kHBytes = QH * 1024, kStage = (QH + QW) * 1024 + (H8 ? 256 : 0);
+    constexpr int kRing = NW * S * kStage, kParts = NW * TILE * (OUTS + 1) * 4;
+    __shared__ __attribute__((aligned(128))) char lds[kRing > kParts ? kRing : kParts];
+    __shared__ int list[TILE];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l16 = lane & 15, quad = lane >> 4;
+    const int jt = (p.n + OUTS - 1) / OUTS;
+    const int t = (int)(blockIdx.x / (unsigned)jt), j0 = (int)(blockIdx.x % (unsigned)jt) * OUTS;
+    TileOf tile{0, p.rows - t * TILE < TILE ? p.rows - t * TILE : TILE, 0, 0};
+    if constexpr (ROUTED) {
+        tile = routed_tile<TILE>(p, t);
+        if (tile.expert == -2) return;
+    }
+    auto slot_of = [&](int i) { return ROUTED ? list[i] : t * TILE + i; };      // the i-th slot of the tile
+    f32x4 acc[MT][JT];
+#pragma unroll
+    for (int m = 0; m < MT; m++)
+#pragma unroll
+        for (int j = 0; j < JT; j++) acc[m][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+    if (!ROUTED || tile.expert >= 0) {
+        const int nk = (p.cols + kStep - 1) / kStep, nb = (p.cols + kScaleBlock - 1) / kScaleBlock, nb4 = up_to(nb, 4);
+        const long long kp = (long long)nb * kScaleBlock, wpitch = W8 ? kp : 2ll * p.cols, hpitch = H8 ? kp : 2ll * p.cols;
+        const unsigned char* W = operand<unsigned char>(p.W, p.slots, 0);
+        const unsigned char* h = operand<unsigned char>(p.h, p.slots, 1);
+        const float* scales = (const float*)(W + (long long)p.experts * p.n * kp) + ((long long)tile.expert * ((p.n + kScaleBlock - 1) / kScaleBlock) + j0 / kScaleBlock) * nb;
+        const int hrows = ROUTED && p.per_slot ? p.rows * p.k : p.rows;
+        auto hrow = [&](int i) { const int s = slot_of(i < tile.used ? i : tile.used - 1); return (long long)(ROUTED && !p.per_slot ? s / p.k : s); };
+        // lane l of a load takes the 16-byte piece (l & 7) ^ (l >> 3) of row l >> 3 of its eight: fragment reads of eight lanes touch every bank once
+        const int piece = (lane & 7) ^ (lane >> 3);
+        const unsigned char *hp[MT * 2], *wp[QW], *hs = h;
+#pragma unroll
+        for (int q = 0; q < QW; q++) {
+            const int j = j0 + q * 8 + (lane >> 3);
+            wp[q] = W + ((long long)tile.expert * p.n + (j < p.n ? j : p.n - 1)) * wpitch;
+        }
+        char* const mine = lds + wave * (S * kStage);
+        const unsigned mine0 = lds_address(mine);
+        const int f0 = l16 * 128 + ((quad ^ (l16 & 7)) * 16), f1 = l16 * 128 + (((quad + 4) ^ (l16 & 7)) * 16);
+        const int g0 = HS == 1 ? f0 : l16 * 128 + (((2 * quad) ^ (l16 & 7)) * 16), g1 = HS == 1 ? f1 : l16 * 128 + (((2 * quad + 1) ^ (l16 & 7)) * 16);
+        // The wave's steps: wave, wave + NW, ..., begun at another place by neighbouring workgroups of an XCD (rows of a power of two long have a
+        // column in few memory channels).  By the outputs alone: a slot's sums may not depend on the tile that it is sorted into.
+        const int turn = (int)((unsigned)(j0 / OUTS >> 3) * NW % (unsigned)nk), mine_n = (nk - wave + NW - 1) / NW;
+        auto step = [&](int b) { const int k = wave + NW * b + turn; return k < nk ? k : k - nk; };
+        // way: 0 straight into LDS; 1 by way of registers; 2 the same, rows shorter than 16 bytes
+        auto bf16_piece = [&](auto way, const unsigned char* row, int k, int more, char* dst) {
+            constexpr int kWay = decltype(way)::value;
+            const int c = k * kStep + more + piece * 8;
+            if constexpr (kWay == 0) direct_to_lds((k + 1) * kStep <= p.cols || c < p.cols ? row + 2ll * c : (const unsigned char*)kZeros, dst);
+            else *(v4u*)(dst + lane * 16) = kWay == 1 ? row8_shifted((const bf16_t*)row, c, p.cols) : row8_short((const bf16_t*)row, c, p.cols);
+        };
+        auto issue_weights = [&](auto way, int b, char* to) {
+            const int k = step(b);
+#pragma unroll
+            for (int q = 0; q < QW; q++) {
+                if constexpr (W8) direct_to_lds(wp[q] + (long long)k * 128 + piece * 16, to + kHBytes + q * 1024);
+                else bf16_piece(way, wp[q], k, 0, to + kHBytes + q * 1024);
+            }
+        };
+        auto issue_rows = [&](auto way, int b, char* to) {
+            const int k = step(b);
+            if constexpr (H8) word_to_lds(hs + (k & ~3), to + kHBytes + QW * 1024);
+#pragma unroll
+            for (int q = 0; q < QH; q++) {
+                if constexpr (H8) direct_to_lds(hp[q] + (long long)k * 128 + piece * 16, to + q * 1024);
+                else bf16_piece(way, hp[q % (MT * 2)], k, q / (MT * 2) * 64, to + q * 1024);
+            }
+        };
+        float scale64 = 0.f;                                   // lane l: the scale of the wave's step l of 64
+        auto load_scales = [&](int b) { if (W8) scale64 = *(const float PG_GLOBAL*)(uintptr_t)(scales + step(b + lane < mine_n ? b + lane : mine_n - 1)); };
+        auto stream = [&](auto way) {
+            constexpr bool kDirect = decltype(way)::value == 0;
+            constexpr int kAhead = kDirect ? S : 1;
+            if (mine_n > 0) {
+                load_scales(0);
+#pragma unroll
+                for (int b = 0; b < kAhead; b++) if (b < mine_n) issue_weights(way, b, mine + b * kStage);
+            }
+            if constexpr (ROUTED) tile_slots<TILE>(p, tile, list);          // (the weights are on their way meanwhile)
+#pragma unroll
+            for (int q = 0; q < MT * 2; q++) hp[q] = h + hrow(q * 8 + (lane >> 3)) * hpitch;
+            if constexpr (H8) hs = h + hrows * kp + hrow(lane % TILE) * nb4;
+#pragma unroll
+            for (int b = 0; b < kAhead; b++) if (b < mine_n) issue_rows(way, b, mine + b * kStage);
+            asm volatile("" : "+v"(scale64));                  // (waits for the scales here, not at each use for whatever was loaded behind them)
+            int at = 0;
+#pragma unroll 1
+            for (int b = 0; b < mine_n; b++) {
+                if (W8 && b && (b & 63) == 0) {
+                    load_scales(b);
+                    asm volatile("" : "+v"(scale64));
+                }
+                if (kAhead > 1 && b && b + kAhead <= mine_n) wait_loads<(kAhead - 1) * kLoads>();      // (at first rows come behind all steps' weights)
+                else wait_loads<0>();
+                const unsigned now = mine0 + (unsigned)at;
+                unsigned exps[MT];
+                if constexpr (H8) lds_bytes<MT>(now + kHBytes + QW * 1024 + l16 * 4 + (step(b) & 3), exps);
+                v4u hf[HS][MT][2], wf[JT][2];
+#pragma unroll
+                for (int q = 0; q < HS; q++) lds_frags<MT>(now + q * MT * 2048 + g0, now + q * MT * 2048 + g1, hf[q]);
+                lds_frags<JT>(now + kHBytes + f0, now + kHBytes + f1, wf);
+                if (b + kAhead < mine_n) {                     // (what was there has been read)
+                    issue_weights(way, b + kAhead, mine + at);
+                    issue_rows(way, b + kAhead, mine + at);
+                }
+                at = kAhead == 1 || at + kStage == S * kStage ? 0 : at + kStage;
+                const float s = W8 ? __int_as_float(__builtin_amdgcn_readlane(__float_as_int(scale64), b & 63)) : 1.f;
+#pragma unroll
+                for (int j = 0; j < JT; j++) {
+                    if constexpr (FORM == kW8H8) {
+                        const v4u a0 = wf[j][0], a1 = wf[j][1];
+                        const v8i A = {(int)a0.x, (int)a0.y, (int)a0.z, (int)a0.w, (int)a1.x, (int)a1.y, (int)a1.z, (int)a1.w};
+#pragma unroll
+                        for (int m = 0; m < MT; m++) {
+                            const v4u b0 = hf[0][m][0], b1 = hf[0][m][1];
+                            const v8i B = {(int)b0.x, (int)b0.y, (int)b0.z, (int)b0.w, (int)b1.x, (int)b1.y, (int)b1.z, (int)b1.w};
+                            const f32x4 sum = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(A, B, f32x4{0.f, 0.f, 0.f, 0.f}, 0, 0, 0, 127, 0, (int)exps[m]);
+#pragma unroll
+                            for (int i = 0; i < 4; i++) acc[m][j][i] = __builtin_fmaf(s, sum[i], acc[m][j][i]);
+                        }
+                    } else if constexpr (FORM == kW16H16) {
+#pragma unroll
+                        for (int m = 0; m < MT; m++)
+#pragma unroll
+                            for (int q = 0; q < 2; q++) acc[m][j] = mfma_bf16(wf[j][q], hf[0][m][q], acc[m][j]);
+                    } else {
+                        v4u A[4];
+#pragma unroll
+                        for (int q = 0; q < 4; q++) A[q] = half_to_bf16(wf[j][q >> 1], q & 1);
+#pragma unroll
+                        for (int m = 0; m < MT; m++) {
+                            f32x4 sum = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                            for (int q = 0; q < 4; q++) sum = mfma_bf16(A[q], H8 ? half_to_bf16(hf[0][m][q >> 1], q & 1) : hf[HS == 2 ? q >> 1 : 0][m][q & 1], sum);
+                            const float by = H8 ? __builtin_ldexpf(s, (int)exps[m] - 127) : s;
+#pragma unroll
+                            for (int i = 0; i < 4; i++) acc[m][j][i] = __builtin_fmaf(by, sum[i], acc[m][j][i]);
+                        }
+                    }
+                }
+            }
+        };
+        // (uniform) can 16-byte loads into LDS reach the bf16 rows?
+        if ((W8 && H8) || (p.cols % 8 == 0 && aligned_to(h, 16) && (W8 || aligned_to(W, 16)))) stream(std::integral_constant<int, 0>{});
+        else if constexpr (!(W8 && H8)) {
+            if (MT > 1 || JT > 1 || p.cols >= 8) stream(std::integral_constant<int, 1>{});
+            else if constexpr (MT == 1 && JT == 1) stream(std::integral_constant<int, 2>{});         // (plan_experts)
+        }
+    } else if constexpr (ROUTED) {
+        tile_slots<TILE>(p, tile, list);
+    }
+    __syncthreads();                                           // every wave has read its steps
+    float* const part = (float*)lds;                           // [NW][TILE][OUTS + 1]
+#pragma unroll
+    for (int m = 0; m < MT; m++)
+#pragma unroll
+        for (int j = 0; j < JT; j++)
+#pragma unroll
+            for (int i = 0; i < 4; i++) part[(wave * TILE + m * 16 + l16) * (OUTS + 1) + j * 16 + quad * 4 + i] = acc[m][j][i];
+    __syncthreads();
+    for (int i = threadIdx.x; i < TILE * OUTS; i += NW * 64) {
+        const int m = i / OUTS, c = i % OUTS;
+        if (m >= tile.used || j0 + c >= p.n) continue;
+        float y = part[m * (OUTS + 1) + c];
+#pragma unroll
+        for (int w = 1; w < NW; w++) y += part[(w * TILE + m) * (OUTS + 1) + c];
+        const long long at = (long long)slot_of(m) * p.n + j0 + c;
+        if (p.out_f32) ((float*)p.out)[at] = y;
+        else ((bf16_t*)p.out)[at] = (bf16_t)f32_to_bf16(y);
+    }
+}
+
+// ---- large products -----------------------------------------------------------------------------------------
+// Workgroup b of `total` in an order that gives each of the eight XCDs (workgroups go to them in turn) a stretch of neighbours: they share
+// rows and weights in its L2.
+__device__ __forceinline__ unsigned neighbours(unsigned b, unsigned total) {
+    const unsigned x = b & 7u, each = total >> 3, more = total & 7u;
+    return x * each + (x < more ? x : more) + (b >> 3);
+}
+// WR x WJ waves, each RM x JN tiles of 16 rows x 16 outputs, over K in steps of 128 columns (64 where the weights are bf16), S steps in LDS: S - 1 on
+// their way while one is multiplied.
+template <Form FORM, bool ROUTED, int RM, int JN, int WR, int WJ, int S>
 __global__ __launch_bounds__(WR * WJ * 64, 2) void k_product_tile(ExpertArgs p) {
     constexpr bool W8 = FORM != kW16H16, H8 = FORM == kW8H8 || FORM == kW8H8Wide;
     constexpr int NW = WR * WJ, BM = RM * 16 * WR, BN = JN * 16 * WJ;
@@ -555,9 +710,11 @@ __global__ __launch_bounds__(WR * WJ * 64, 2) void k_product_tile(ExpertArgs p) 
     constexpr int kHBytes = HS * BM * 128, kStage = kHBytes + BN * 128;
     constexpr int QH = HS * BM / 8 / NW, QW = BN / 8 / NW;    // loads of eight rows for each wave
     static_assert(QH * 8 * NW == HS * BM && QW * 8 * NW == BN && (128 % (JN * 16)) == 0, "whole loads; a wave's outputs share their scale");
-    __shared__ __attribute__((aligned(128))) char lds[2 * kStage];
+    constexpr int kLoads = QH + QW + (H8 ? 1 : 0);            // a wave's loads of a step
+    static_assert(S >= 2 && S <= 8 && BM % 64 == 0, "exponents: of four steps at a time, in four places");
+    __shared__ __attribute__((aligned(128))) char lds[S * kStage];
     __shared__ int slot_of[BM];
-    __shared__ __attribute__((aligned(16))) char lds_exps[2][H8 ? BM * 4 : 16];       // of four steps each
+    __shared__ __attribute__((aligned(16))) char lds_exps[4][H8 ? BM * 4 : 16];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), l16 = lane & 15, quad = lane >> 4;
     const int jt = (p.n + BN - 1) / BN;
     int t, jb;
@@ -573,19 +730,17 @@ __global__ __launch_bounds__(WR * WJ * 64, 2) void k_product_tile(ExpertArgs p) 
             jb = (int)(in / rows4);
         }
     }
-    int expert = 0, begin = t * BM, used = p.rows - begin < BM ? p.rows - begin : BM;
+    const int begin = t * BM;
+    TileOf tile{0, p.rows - begin < BM ? p.rows - begin : BM, 0, 0};
     if constexpr (ROUTED) {
-        if (t >= ((const SortedSlots*)p.sorted)->n_tiles) return;
-        const SortedTile st = sorted_tiles(p.sorted)[t];
-        expert = st.expert;
-        begin = st.begin;
-        used = st.end - st.begin;
+        tile = routed_tile<BM>(p, t);
+        if (tile.expert == -2) return;
+        tile_slots<BM>(p, tile, slot_of);
+    } else {
+        for (int i = lane; i < BM; i += 64) slot_of[i] = begin + (i < tile.used ? i : tile.used - 1);
+        __builtin_amdgcn_wave_barrier();
     }
-    for (int i = tid; i < BM; i += NW * 64) {
-        const int at = begin + (i < used ? i : used - 1);
-        slot_of[i] = ROUTED ? sorted_order(p.sorted, p.tiles)[at] : at;
-    }
-    __syncthreads();
+    const int expert = tile.expert, used = tile.used;
     const int j0 = jb * BN, wr = wave / WJ, wj = wave % WJ;      // (waves w and w + 4 share a SIMD: other rows, of which a small tile may have none)
     const int nk = (p.cols + kStep - 1) / kStep, nb = (p.cols + kScaleBlock - 1) / kScaleBlock, nb4 = up_to(nb, 4);
     const long long kp = (long long)nb * kScaleBlock;
@@ -618,15 +773,18 @@ __global__ __launch_bounds__(WR * WJ * 64, 2) void k_product_tile(ExpertArgs p) 
             const int j = (wave * QW + q) * 8 + (lane >> 3), last = p.n - 1 - j0;
             wp[q] = (unsigned)(j < last ? j : last) * (unsigned)wpitch + (W8 ? piece * 16 : 0);
         }
-        const unsigned exps_at = H8 && wave < BM / 64 ? hrow(wave * 64 + lane) * (unsigned)nb4 : 0u;
-        auto load_exps = [&](int k) {                          // k: a multiple of four
-            if (wave < BM / 64) word_to_lds(hs + k, exps_at, lds_exps[(k >> 2) & 1] + wave * 256);
-        };
+        // the word of a row's exponents that step k's is in; every wave has a load of every step, so that all count the same
+        const int exps_rows = wave % (BM / 64);
+        const unsigned exps_at = H8 ? hrow(exps_rows * 64 + lane) * (unsigned)nb4 : 0u;
+        auto load_exps = [&](int k) { word_to_lds(hs + (k & ~3), exps_at, lds_exps[(k >> 2) & 3] + exps_rows * 256); };
         // (uniform) can 16-byte loads into LDS reach the bf16 rows?
         const bool direct = (W8 && H8) || (p.cols % 8 == 0 && aligned_to(h, 16) && (W8 || aligned_to(W, 16)));
         constexpr int kRegs = (H8 ? 0 : QH) + (W8 ? 0 : QW);
         v4u held[kRegs ? kRegs : 1];
-        auto issue = [&](int k, char* to) {
+        auto issue = [&](auto way, int k, char* to) {
+            constexpr bool kDirect = decltype(way)::value;
+            const bool inside = (k + 1) * kStep <= p.cols;     // (uniform)
+            if constexpr (H8) load_exps(k);
 #pragma unroll
             for (int q = 0; q < QH; q++) {
                 const int at = (wave * QH + q) * 8;          // of HS * BM pieces of rows
@@ -635,8 +793,10 @@ __global__ __launch_bounds__(WR * WJ * 64, 2) void k_product_tile(ExpertArgs p) 
                     direct_to_lds(h + (long long)k * 128, hp[q], dst);
                 } else {
                     const int c = k * kStep + (at / BM) * 64 + piece * 8;
-                    if (direct) direct_to_lds(c < p.cols ? h + hp[q] + 2ll * c : (const unsigned char*)kZeros, dst);
-                    else held[q] = row8_shifted((const bf16_t*)(h + hp[q]), c, p.cols);
+                    if constexpr (kDirect) {
+                        if (inside) direct_to_lds(h + 2ll * k * kStep, hp[q] + (unsigned)((at / BM) * 128 + piece * 16), dst);
+                        else direct_to_lds(c < p.cols ? h + hp[q] + 2ll * c : (const unsigned char*)kZeros, dst);
+                    } else held[q] = row8_shifted((const bf16_t*)(h + hp[q]), c, p.cols);
                 }
             }
 #pragma unroll
@@ -646,14 +806,16 @@ __global__ __launch_bounds__(WR * WJ * 64, 2) void k_product_tile(ExpertArgs p) 
                     direct_to_lds(W + (long long)k * 128, wp[q], dst);
                 } else {
                     const int c = k * kStep + piece * 8;
-                    if (direct) direct_to_lds(c < p.cols ? W + wp[q] + 2ll * c : (const unsigned char*)kZeros, dst);
-                    else held[(H8 ? 0 : QH) + q] = row8_shifted((const bf16_t*)(W + wp[q]), c, p.cols);
+                    if constexpr (kDirect) {
+                        if (inside) direct_to_lds(W + 2ll * k * kStep, wp[q] + piece * 16u, dst);
+                        else direct_to_lds(c < p.cols ? W + wp[q] + 2ll * c : (const unsigned char*)kZeros, dst);
+                    } else held[(H8 ? 0 : QH) + q] = row8_shifted((const bf16_t*)(W + wp[q]), c, p.cols);
                 }
             }
         };
-        auto put_held = [&](char* to) {
-            if constexpr (kRegs) {
-                if (!direct) {
+        auto put_held = [&](auto way, char* to) {
+            if constexpr (kRegs && !decltype(way)::value) {
+                {
                     if constexpr (!H8)
 #pragma unroll
                         for (int q = 0; q < QH; q++) *(v4u*)(to + (wave * QH + q) * 1024 + lane * 16) = held[q];
@@ -671,28 +833,34 @@ __global__ __launch_bounds__(WR * WJ * 64, 2) void k_product_tile(ExpertArgs p) 
         float scale64 = 0.f;
         auto load_scales = [&](int k) { if (W8) scale64 = *(const float PG_GLOBAL*)(uintptr_t)(scales + (k + lane < nb ? k + lane : nb - 1)); };
         load_scales(0);
-        if constexpr (H8) load_exps(0);
-        const unsigned lds0 = lds_address(lds);
+        const unsigned lds0 = lds_address(lds), exps0 = lds_address(lds_exps[0]) + (wr * RM * 16 + l16) * 4;
         constexpr int kPer = FORM == kW8H8 || FORM == kW16H16 ? 2 : 1;       // tiles of weights that are read at a time
-        issue(0, lds);
-        put_held(lds);
+        auto stream = [&](auto way) {
+        constexpr int kAhead = decltype(way)::value ? S - 1 : 1;             // (rows that come through registers: one step)
+#pragma unroll
+        for (int k = 0; k < kAhead; k++) if (k < nk) issue(way, k, lds + k * kStage);
+        put_held(way, lds);
+        // (the compiler waits for the scales here, and not at each of their uses for whatever was loaded behind them)
+        asm volatile("" : "+v"(scale64));
+        int now_at = 0, next_at = kAhead * kStage;             // in LDS: this step, and the one to load
 #pragma unroll 1
         for (int k = 0; k < nk; k++) {
-            char* const next = lds + ((k + 1) & 1) * kStage;
-            __builtin_amdgcn_s_waitcnt(0x0f70);                // vmcnt(0): this wave's loads of this step
-            __syncthreads();
-            unsigned exps[RM];
-            if constexpr (H8)
-#pragma unroll
-                for (int i = 0; i < RM; i++) exps[i] = (unsigned char)lds_exps[(k >> 2) & 1][((wr * RM + i) * 16 + l16) * 4 + (k & 3)];
-            if (k + 1 < nk) {
-                issue(k + 1, next);
-                if constexpr (H8)
-                    if ((k & 3) == 3) load_exps(k + 1);
+            char* const next = lds + next_at;
+            if (W8 && k && (k & 63) == 0) {
+                load_scales(k);
+                asm volatile("" : "+v"(scale64));
             }
+            // this wave's loads of this step, which came before those of the steps behind it
+            if (kAhead > 1 && k + kAhead - 1 < nk) wait_loads<(kAhead - 1) * kLoads>();
+            else wait_loads<0>();
+            lds_barrier();                                     // all waves' loads of this step are in, and the step before has been read
+            if (k + kAhead < nk) issue(way, k + kAhead, next);
             const float s = W8 ? __int_as_float(__builtin_amdgcn_readlane(__float_as_int(scale64), k & 63)) : 1.f;
-            if (W8 && (k & 63) == 63) load_scales(k + 1);
-            const unsigned now = lds0 + (unsigned)(k & 1) * kStage;
+            const unsigned now = lds0 + (unsigned)now_at;
+            now_at = now_at + kStage == S * kStage ? 0 : now_at + kStage;
+            next_at = next_at + kStage == S * kStage ? 0 : next_at + kStage;
+            unsigned exps[RM];
+            if constexpr (H8) lds_bytes<RM>(exps0 + ((k >> 2) & 3) * (BM * 4) + (k & 3), exps);
             if (wr * RM * 16 < used) {
             v4u hf[HS][RM][2];
 #pragma unroll
@@ -738,8 +906,11 @@ __global__ __launch_bounds__(WR * WJ * 64, 2) void k_product_tile(ExpertArgs p) 
                 }
             }
             }
-            put_held(next);
+            put_held(way, next);
         }
+        };
+        if ((W8 && H8) || direct) stream(std::true_type{});
+        else if constexpr (!(W8 && H8)) stream(std::false_type{});
     }
     // Out by whole pieces of rows: 16 rows of a wave at a time go through its own part of LDS (16 bytes between rows: other banks), 16 bytes a lane from there.
     __builtin_amdgcn_s_waitcnt(0x0f70);
@@ -747,7 +918,7 @@ __global__ __launch_bounds__(WR * WJ * 64, 2) void k_product_tile(ExpertArgs p) 
     auto emit = [&](auto* out) {
         using O = std::remove_pointer_t<decltype(out)>;
         constexpr int NV = 16 / (int)sizeof(O), kPitch = JN * 16 * (int)sizeof(O) + 16, kLanes = JN * 16 / NV, kRowsAt = 64 / kLanes;
-        static_assert(NW * 16 * kPitch <= 2 * kStage, "the waves' parts");
+        static_assert(NW * 16 * kPitch <= S * kStage, "the waves' parts");
         char* const mine = lds + wave * 16 * kPitch;
         const int c = j0 + wj * JN * 16 + lane % kLanes * NV;
 #pragma unroll
@@ -791,14 +962,29 @@ struct TileKernel {
     const void* routed;
     int rows, outputs, threads, from;        // from: workgroups
 };
-#define PG_TILE(F, RM, JN, WR, WJ, FROM) {F, PG_FN(k_product_tile<F, false, RM, JN, WR, WJ>), PG_FN(k_product_tile<F, true, RM, JN, WR, WJ>), RM * 16 * WR, JN * 16 * WJ, WR * WJ * 64, FROM}
+#define PG_TILE(F, RM, JN, WR, WJ, S, FROM) {F, PG_FN(k_product_tile<F, false, RM, JN, WR, WJ, S>), PG_FN(k_product_tile<F, true, RM, JN, WR, WJ, S>), RM * 16 * WR, JN * 16 * WJ, WR * WJ * 64, FROM}
 const TileKernel kTileKernels[] = {
-    PG_TILE(kW8H8, 4, 8, 4, 2, 128), PG_TILE(kW8H8, 2, 4, 4, 2, 64),
-    PG_TILE(kW8H16, 4, 4, 2, 4, 128), PG_TILE(kW8H16, 2, 4, 4, 2, 64),
-    PG_TILE(kW16H16, 4, 8, 4, 2, 128), PG_TILE(kW16H16, 2, 4, 4, 2, 64),
-    PG_TILE(kW8H8Wide, 4, 4, 2, 4, 128), PG_TILE(kW8H8Wide, 2, 4, 4, 2, 64),
+    PG_TILE(kW8H8, 4, 8, 4, 2, 2, 128), PG_TILE(kW8H8, 2, 4, 4, 2, 4, 128),
+    PG_TILE(kW8H16, 4, 4, 2, 4, 2, 128), PG_TILE(kW8H16, 2, 4, 4, 2, 3, 128),
+    PG_TILE(kW16H16, 4, 8, 4, 2, 2, 128), PG_TILE(kW16H16, 2, 4, 4, 2, 4, 128),
+    PG_TILE(kW8H8Wide, 4, 4, 2, 4, 3, 128), PG_TILE(kW8H8Wide, 2, 4, 4, 2, 4, 128),
 };
 
+struct RowsKernel {
+    Form form;
+    const void* plain;
+    const void* routed;
+    int rows, outputs, threads;
+};
+#define PG_ROWS(F, MT, JT, S, NW) {F, PG_FN(k_product<F, false, MT, JT, S, NW>), PG_FN(k_product<F, true, MT, JT, S, NW>), 16 * MT, 16 * JT, NW * 64}
+const RowsKernel kRowsKernels[] = {
+    PG_ROWS(kW16H16, 1, 1, 4, 4), PG_ROWS(kW16H16, 1, 2, 3, 4), PG_ROWS(kW16H16, 1, 4, 3, 4), PG_ROWS(kW16H16, 2, 1, 3, 4), PG_ROWS(kW16H16, 2, 2, 2, 4), PG_ROWS(kW16H16, 2, 4, 3, 4), PG_ROWS(kW16H16, 4, 1, 3, 4), PG_ROWS(kW16H16, 4, 2, 3, 4), PG_ROWS(kW16H16, 4, 4, 2, 4),
+    PG_ROWS(kW8H16, 1, 1, 3, 4), PG_ROWS(kW8H16, 1, 2, 2, 4), PG_ROWS(kW8H16, 1, 4, 3, 4), PG_ROWS(kW8H16, 2, 1, 3, 4), PG_ROWS(kW8H16, 2, 2, 3, 4), PG_ROWS(kW8H16, 2, 4, 2, 4), PG_ROWS(kW8H16, 4, 1, 2, 4), PG_ROWS(kW8H16, 4, 2, 1, 4), PG_ROWS(kW8H16, 4, 4, 1, 4),
+    PG_ROWS(kW8H8, 1, 1, 4, 4), PG_ROWS(kW8H8, 1, 2, 3, 4), PG_ROWS(kW8H8, 1, 4, 3, 4), PG_ROWS(kW8H8, 2, 1, 3, 4), PG_ROWS(kW8H8, 2, 2, 2, 4), PG_ROWS(kW8H8, 2, 4, 3, 4), PG_ROWS(kW8H8, 4, 1, 3, 4), PG_ROWS(kW8H8, 4, 2, 3, 4), PG_ROWS(kW8H8, 4, 4, 2, 4),
+    PG_ROWS(kW8H8Wide, 1, 1, 4, 4), PG_ROWS(kW8H8Wide, 1, 2, 3, 4), PG_ROWS(kW8H8Wide, 1, 4, 3, 4), PG_ROWS(kW8H8Wide, 2, 1, 3, 4), PG_ROWS(kW8H8Wide, 2, 2, 2, 4), PG_ROWS(kW8H8Wide, 2, 4, 3, 4), PG_ROWS(kW8H8Wide, 4, 1, 3, 4), PG_ROWS(kW8H8Wide, 4, 2, 3, 4), PG_ROWS(kW8H8Wide, 4, 4, 2, 4),
+};
+
+constexpr long long kRowsFrom = 256;
 constexpr long long kSmallestTile = 16;
 long long most_tiles(long long slots, long long experts, long long tile) { return slots / tile + std::min(slots, experts + 1); }
 
@@ -807,6 +993,7 @@ long long most_tiles(long long slots, long long experts, long long tile) { retur
 size_t sorted_bytes(int op, const Shape& s) {
     if (op != kExpertGemv || s.rows < 1 || s.m < 1 || s.m > (1 << 24) / s.rows || s.inner < 1 || s.inner > kSortMostExperts) return 0;
     const long long slots = s.rows * s.m;
+    if (slots <= kFewSlots) return 0;
     return sizeof(SortedSlots) + (size_t)most_tiles(slots, s.inner, kSmallestTile) * sizeof(SortedTile) + (size_t)slots * sizeof(int);
 }
 
@@ -842,10 +1029,10 @@ bool plan_experts(int op, int dtype, const Shape& s, Launch* out, Launch* pre) {
         const bool routed = op == kExpertGemv, w8 = s.in_dtype[0] == kF8Weight, h8 = s.in_dtype[1] == kF8Rows;
         const long long slots = routed ? s.rows * s.m : s.rows;
         const Form form = !w8 ? kW16H16 : !h8 ? kW8H16 : f32 ? kW8H8Wide : kW8H8;
-        auto with = [&](int tile, int outputs) {
+        auto with = [&](int tile, int outputs, bool in_pairs = false) {
             out->tile = tile;
             out->tiles = (int)(routed ? most_tiles(slots, s.inner, tile) : (slots + tile - 1) / tile);
-            const long long grid = (routed && tile > kSmallestTile ? (out->tiles + 15) / 16 * 16 : out->tiles) * ((s.n + outputs - 1) / outputs);
+            const long long grid = (in_pairs ? (out->tiles + 15) / 16 * 16 : out->tiles) * ((s.n + outputs - 1) / outputs);
             out->grid = dim3((unsigned)grid);
             return grid <= 0x7fffffffll;
         };
@@ -855,18 +1042,23 @@ bool plan_experts(int op, int dtype, const Shape& s, Launch* out, Launch* pre) {
         const long long pitch = w8 ? (s.cols + kScaleBlock - 1) / kScaleBlock * kScaleBlock : 2 * s.cols, hpitch = h8 ? pitch : 2 * s.cols;
         const bool fits = s.cols >= 8 && 256 * std::max(pitch, hpitch) < (1ll << 32) && (!routed || slots * hpitch < (1ll << 32));
         for (const TileKernel& k : kTileKernels)
-            if (k.form == form && fits && (!routed || 2 * slots / s.inner >= k.rows) && (slots / (routed ? s.inner : 1) + k.rows - 1) / k.rows * (routed ? s.inner : 1) * ((s.n + k.outputs - 1) / k.outputs) >= k.from) { fit = &k; break; }
+            if (k.form == form && fits && 2 * slots / (routed ? s.inner : 1) >= k.rows && (slots / (routed ? s.inner : 1) + k.rows - 1) / k.rows * (routed ? s.inner : 1) * ((s.n + k.outputs - 1) / k.outputs) >= k.from) { fit = &k; break; }
         if (fit) {
-            if (!with(fit->rows, fit->outputs)) return false;
+            if (!with(fit->rows, fit->outputs, routed)) return false;
             out->fn = routed ? fit->routed : fit->plain;
             out->block = dim3(fit->threads);
         } else {
-            if (!with((int)kSmallestTile, 16)) return false;
-            out->fn = routed ? (form == kW16H16 ? PG_FN(k_product<kW16H16, true>) : form == kW8H16 ? PG_FN(k_product<kW8H16, true>)
-                                : form == kW8H8 ? PG_FN(k_product<kW8H8, true>) : PG_FN(k_product<kW8H8Wide, true>))
-                             : (form == kW8H16 ? PG_FN(k_product<kW8H16, false>) : form == kW8H8 ? PG_FN(k_product<kW8H8, false>) : PG_FN(k_product<kW8H8Wide, false>));
+            const long long each = routed ? (slots + std::min(slots, s.inner) - 1) / std::min(slots, s.inner) : slots;      // slots of an expert, about
+            // the smallest tile that holds an expert's rows, up to 64 of them, with as many outputs as leave kRowsFrom workgroups
+            const RowsKernel* k = kRowsKernels;
+            while (k->form != form || (s.cols >= 8 && each > k->rows && k->rows < 64)) k++;
+            const long long about = routed ? std::min(slots, s.inner) * ((each + k->rows - 1) / k->rows) : (slots + k->rows - 1) / k->rows;
+            while (s.cols >= 8 && k->outputs < 64 && about * ((s.n + k[1].outputs - 1) / k[1].outputs) >= kRowsFrom) k++;
+            if (!with(k->rows, k->outputs)) return false;
+            out->fn = routed ? k->routed : k->plain;
+            out->block = dim3(k->threads);
         }
-        if (routed) {
+        if (routed && slots > kFewSlots) {
             pre->fn = PG_FN(k_sort_slots);
             pre->arg_bytes = sizeof(ExpertArgs);
             pre->block = dim3(kSortThreads);
