@@ -88,8 +88,8 @@ typedef enum {
  * PG_ROUTE        in: s [rows, cols], dtype PG_F32 or PG_BF16, and optionally bias [cols] PG_F32 (PG_REF_NONE: zeros); out: PG_ROUTED [rows, n];
  *                 rows, cols = experts (1 to 1024), n = slots a row (1 to 64, <= cols); m = groups (0 or 1: none; divides cols, <= 64) and
  *                 inner = how many of them are kept (1 to m); eps = a factor of the weights (0: 1); flags.
- *                 p = softmax of s over the row, or sigmoid(s) (PG_ROUTE_SIGMOID); experts are compared by c = p + bias, evaluated in 64 bits,
- *                 equal ones by the lower index.  A group counts as its best c, or as the sum of its two best (PG_ROUTE_GROUP_TOP2); the
+ *                 p = softmax of s over the row, or sigmoid(s) (PG_ROUTE_SIGMOID); experts are compared by c = p + bias, evaluated in 64 bits, or
+ *                 without a bias by their scores, which are in the order of p; equal ones by the lower index.  A group counts as its best c, or as the sum of its two best (PG_ROUTE_GROUP_TOP2); the
  *                 `inner` best groups stay.  The slots hold the n best experts of those, best first, each with the weight p, divided
  *                 by the sum of the chosen p (PG_ROUTE_RENORMALIZE; 0 if that is 0), times the factor.  An expert whose score is -infinity or not a
  *                 number, or whose bias is, is never chosen and counts as nothing; +infinity counts as the largest fp32 number.  Where

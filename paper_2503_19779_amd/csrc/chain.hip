@@ -970,6 +970,7 @@ pg_status make_records(pg_chain* c) {
         }
         pgk::Shape sh = shape_of(d);
         if (d.op > PG_SCALE_BIAS_RELU) {
+            sh.high = d.op == PG_ROUTE && (d.in[1].kind != PG_REF_NONE || (d.m > 1 && (d.flags & PG_ROUTE_GROUP_TOP2)));
             for (int j = 0; j < 2 && j < r.n_in; j++)
                 if (d.in[j].kind != PG_REF_NONE)
                     sh.in_dtype[j] = (d.in[j].kind == PG_REF_EXT ? c->ext[d.in[j].index] : d.in[j].kind == PG_REF_INT ? c->ints[d.in[j].index] : c->w[d.in[j].index]).dtype;

@@ -167,7 +167,6 @@ __global__ __launch_bounds__(kBlock) void k_expert_sum(ExpertSumArgs p) {
 }
 
 // ---- PG_ROUTE ----------------------------------------------------------------------------------------------
-__device__ __forceinline__ double dmax(double a, double b) { return a > b ? a : b; }
 template <int CTRL> __device__ __forceinline__ double dpp_take64(double v) {
     const unsigned long long u = __builtin_bit_cast(unsigned long long, v);
     const unsigned lo = (unsigned)__builtin_amdgcn_update_dpp(0, (int)(unsigned)u, CTRL, 0xf, 0xf, false);
@@ -179,111 +178,263 @@ __device__ __forceinline__ double read_lane64(double v, int lane) {
     const unsigned lo = (unsigned)__builtin_amdgcn_readlane((int)(unsigned)u, lane), hi = (unsigned)__builtin_amdgcn_readlane((int)(unsigned)(u >> 32), lane);
     return __builtin_bit_cast(double, (unsigned long long)hi << 32 | lo);
 }
-template <class Op> __device__ __forceinline__ double wave_all64(double v, Op op) {
-    v = op(v, dpp_take64<0xB1>(v));
-    v = op(v, dpp_take64<0x4E>(v));
-    v = op(v, dpp_take64<0x141>(v));
-    v = op(v, dpp_take64<0x140>(v));
-    return op(op(read_lane64(v, 0), read_lane64(v, 16)), op(read_lane64(v, 32), read_lane64(v, 48)));
+__device__ __forceinline__ float read_lane(float v, int lane) { return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(v), lane)); }
+__device__ __forceinline__ double read_lane_k(double v, int lane) { return read_lane64(v, lane); }
+__device__ __forceinline__ float read_lane_k(float v, int lane) { return read_lane(v, lane); }
+template <int CTRL> __device__ __forceinline__ double dpp_take_k(double v) { return dpp_take64<CTRL>(v); }
+template <int CTRL> __device__ __forceinline__ float dpp_take_k(float v) { return dpp_take<CTRL>(v); }
+__device__ __forceinline__ double wave_sum64(double v) {
+    v += dpp_take64<0xB1>(v);
+    v += dpp_take64<0x4E>(v);
+    v += dpp_take64<0x141>(v);
+    v += dpp_take64<0x140>(v);
+    return (read_lane64(v, 0) + read_lane64(v, 16)) + (read_lane64(v, 32) + read_lane64(v, 48));
+}
+__device__ __forceinline__ float wave_max(float v) {
+    v = row16_max(v);
+    return __builtin_fmaxf(__builtin_fmaxf(read_lane(v, 0), read_lane(v, 16)), __builtin_fmaxf(read_lane(v, 32), read_lane(v, 48)));
+}
+// exp(x) in fp32 within two half steps, x <= 0 or finite: 2^k exp(r), ln 2 in two pieces
+__device__ __forceinline__ float exp_f32(float x) {
+    constexpr float kLog2e = 1.4426950408889634f, kLn2Hi = 0.693145751953125f, kLn2Lo = 1.42860682030941723212e-6f;
+    const float kf = __builtin_rintf(__builtin_fmaxf(__builtin_fminf(x, 100.f), -200.f) * kLog2e);
+    const float r = __builtin_fmaf(kf, -kLn2Lo, __builtin_fmaf(kf, -kLn2Hi, __builtin_fmaxf(__builtin_fminf(x, 100.f), -200.f)));
+    return __builtin_ldexpf(__builtin_amdgcn_exp2f(r * kLog2e), (int)kf);
+}
+// exp of N values in fp64 within about 3e-16, zero and infinite where fp64 is: the sum of r^n / n! to n = 13, |r| <= 0.347 (the next term is below
+// 5e-18).  Side by side: each coefficient takes two moves.
+template <int N>
+__device__ __forceinline__ void exp_f64(double (&x)[N]) {
+    constexpr double kLog2e = 1.4426950408889634, kLn2Hi = 0x1.62e42fefa0000p-1, kLn2Lo = 1.6465949582897082e-12;
+    constexpr double c[] = {1.0 / 6227020800.0, 1.0 / 479001600.0, 1.0 / 39916800.0, 1.0 / 3628800.0, 1.0 / 362880.0, 1.0 / 40320.0, 1.0 / 5040.0,
+                            1.0 / 720.0, 1.0 / 120.0, 1.0 / 24.0, 1.0 / 6.0, 0.5, 1.0, 1.0};
+    double v[N];
+    int e[N];
+#pragma unroll
+    for (int n = 0; n < N; n++) {
+        const double y = __builtin_fmin(__builtin_fmax(x[n], -800.0), 800.0), kf = __builtin_rint(y * kLog2e);
+        x[n] = __builtin_fma(kf, -kLn2Lo, __builtin_fma(kf, -kLn2Hi, y));
+        e[n] = (int)kf;
+        v[n] = c[0];
+    }
+#pragma unroll
+    for (int i = 1; i < 14; i++)
+#pragma unroll
+        for (int n = 0; n < N; n++) v[n] = __builtin_fma(v[n], x[n], c[i]);
+#pragma unroll
+    for (int n = 0; n < N; n++) x[n] = __builtin_ldexp(v[n], e[n]);
+}
+// p of N scores, up to the factor `over`: 1 / (1 + exp(-x)), the reciprocal by two Newton steps and zero below -708, or exp(x - top)
+template <int N>
+__device__ __forceinline__ void scores_p(bool sigmoid, double top, double (&x)[N]) {
+    double d[N];
+#pragma unroll
+    for (int n = 0; n < N; n++) d[n] = sigmoid ? __builtin_fmin(-x[n], 709.0) : x[n] - top;
+    exp_f64(d);
+#pragma unroll
+    for (int n = 0; n < N; n++) {
+        const double q = 1.0 + d[n];
+        double y = __builtin_amdgcn_rcp(q);
+        y = __builtin_fma(__builtin_fma(-q, y, 1.0), y, y);
+        y = __builtin_fma(__builtin_fma(-q, y, 1.0), y, y);
+        x[n] = !sigmoid ? d[n] : x[n] < -708.0 ? 0.0 : y;
+    }
 }
 
-// A wave takes a row, lane l the experts l, l + 64, ...
-template <typename T, int V>
+// A wave takes a row, lane l the experts l * V .. l * V + V - 1.  HIGH: where the choice goes by p itself -- a bias, or sums of two -- p is worked out in
+// fp64; without it the scores are in the order of p, and only the chosen ones need it.  Either way a round of the choice goes by the values rounded to
+// fp32, one instruction a step: what is largest in fp64 is among those that are largest then, mostly the only one.
+template <typename T, int V, bool HIGH>
 __global__ __launch_bounds__(kBlock) void k_route(RouteArgs p) {
-    __shared__ double keys[kBlock / 64][V * 64];
+    using K = std::conditional_t<HIGH, double, float>;
+    __shared__ K shared_keys[kBlock / 64][V * 64 < 128 ? 128 : V * 64];
     const T* s = operand<T>(p.s, p.slots, 0);
     const float* bias = p.bias ? operand<float>(p.bias, p.slots, 1) : nullptr;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const int row = blockIdx.x * (kBlock / 64) + wave;
-    const bool live = row < p.rows;
-    const T* sr = s + (long long)(live ? row : 0) * p.experts;
-    const double none = -__builtin_inf();
-    double x[V], key[V], pr[V];
-    bool ok[V];
-    double top = none;
+    const int row = blockIdx.x * (kBlock / 64) + wave, e0 = lane * V;
+    const bool sigmoid = (p.flags & 1) != 0, two = (p.flags & 4) != 0;
+    if (row >= p.rows) return;                            // (waves share nothing)
+    const T* sr = s + (long long)row * p.experts;
+    constexpr float kNone = -__builtin_inff();
+    float x[V];
+    if (e0 + V <= p.experts) {
+        constexpr int kBytes = V * (int)sizeof(T);
+        unsigned w[kBytes < 4 ? 1 : kBytes / 4];
+        if constexpr (kBytes >= 16) {
+#pragma unroll
+            for (int i = 0; i < kBytes / 16; i++) {
+                const v4u v = *(const v4u_any PG_GLOBAL*)(uintptr_t)((const char*)(sr + e0) + 16 * i);
+                w[4 * i] = v.x; w[4 * i + 1] = v.y; w[4 * i + 2] = v.z; w[4 * i + 3] = v.w;
+            }
+        } else if constexpr (kBytes >= 4) {
+#pragma unroll
+            for (int i = 0; i < kBytes / 4; i++) w[i] = *(const u32_any PG_GLOBAL*)(uintptr_t)((const char*)(sr + e0) + 4 * i);
+        } else {
+            w[0] = load_raw_global(sr + e0);
+        }
+#pragma unroll
+        for (int i = 0; i < V; i++) x[i] = sizeof(T) == 4 ? __uint_as_float(w[i * (int)sizeof(T) / 4]) : __uint_as_float(i & 1 ? w[i / 2] & 0xffff0000u : w[i / 2] << 16);
+    } else {
+#pragma unroll
+        for (int i = 0; i < V; i++) x[i] = e0 + i < p.experts ? load_elem(sr + e0 + i) : kNone;
+    }
+    float top = kNone;
 #pragma unroll
     for (int i = 0; i < V; i++) {
-        const int e = lane + 64 * i;
-        const float f = e < p.experts ? load_elem(sr + e) : -__builtin_inff();
-        ok[i] = f > -__builtin_inff();
-        x[i] = (double)__builtin_fminf(f, 3.40282347e38f);
-        if (ok[i]) top = dmax(top, x[i]);
+        x[i] = x[i] > kNone ? __builtin_fminf(x[i], 3.40282347e38f) : kNone;       // (what is not a number as well)
+        top = __builtin_fmaxf(top, x[i]);
     }
-    top = wave_all64(top, dmax);
-    double total = 0.;
+    top = wave_max(top);
+    // key: what experts are compared by; -inf: never chosen.  p = sigmoid, or exp(x - top) * over
+    K key[V];
+    double pr[HIGH ? V : 1], over = 1.;
+    if constexpr (HIGH) {
+        double total = 0.;
 #pragma unroll
-    for (int i = 0; i < V; i++) {
-        pr[i] = 0.;
-        if (ok[i]) pr[i] = (p.flags & 1) ? 1. / (1. + exp(-x[i])) : exp(x[i] - top);
-        total += pr[i];
-    }
-    if (!(p.flags & 1)) {
-        total = wave_all64(total, [](double a, double b) { return a + b; });
+        for (int i = 0; i < V; i++) pr[i] = (double)x[i];
+        scores_p(sigmoid, (double)top, pr);
 #pragma unroll
-        for (int i = 0; i < V; i++) if (ok[i]) pr[i] = pr[i] / total;
-    }
+        for (int i = 0; i < V; i++) {
+            if (!(x[i] > kNone)) pr[i] = 0.;
+            total += pr[i];
+        }
+        if (!sigmoid) {
+            over = 1. / wave_sum64(total);
 #pragma unroll
-    for (int i = 0; i < V; i++) {
-        const int e = lane + 64 * i;
-        double c = x[i];
-        if (bias && e < p.experts) c = pr[i] + (double)bias[e];
-        key[i] = ok[i] && c > none ? c : none;
+            for (int i = 0; i < V; i++) pr[i] = x[i] > kNone ? pr[i] * over : 0.;
+        }
+#pragma unroll
+        for (int i = 0; i < V; i++) {
+            const double c = bias ? pr[i] + (double)bias[e0 + i < p.experts ? e0 + i : 0] : (double)x[i];
+            key[i] = x[i] > kNone && c > (double)kNone ? c : (double)kNone;
+        }
+    } else {
+        float z = 0.f;
+#pragma unroll
+        for (int i = 0; i < V; i++) {
+            key[i] = x[i];
+            if (!sigmoid) z += x[i] > kNone ? exp_f32(x[i] - top) : 0.f;
+        }
+        if (!sigmoid) over = 1. / (double)wave_sum(z);
     }
     if (p.groups > 1) {
         const int per = p.experts / p.groups;
-        const bool two = (p.flags & 4) != 0;
+        K* const keys = shared_keys[wave];
+        K best = (K)kNone, second = (K)kNone;
+        auto take = [&](K a) {
+            second = a > best ? best : a > second ? a : second;
+            best = a > best ? a : best;
+        };
+        auto counts = [&](int i) -> K {                   // what expert i counts in its group
+            if constexpr (HIGH) { if (two && !bias) return key[i] > (K)kNone ? pr[i] : (K)kNone; }
+            return key[i];
+        };
+        const bool whole = per % V == 0;                  // a group is so many lanes'
+        const int lanes = per / V;
+        const bool rows16 = whole && lanes <= 16 && (lanes & (lanes - 1)) == 0;        // ... of one DPP row
+        if (whole) {
 #pragma unroll
-        for (int i = 0; i < V; i++) keys[wave][lane + 64 * i] = key[i] > none ? (two && !bias ? pr[i] : key[i]) : none;
-        __syncthreads();
-        double best = none, second = none;
-        if (lane < p.groups)
-            for (int i = 0; i < per; i++) {
-                const double v = keys[wave][lane * per + i];
-                if (v > best) { second = best; best = v; }
-                else if (v > second) second = v;
+            for (int i = 0; i < V; i++) take(counts(i));
+        }
+        int from = 1;                                     // the lane that has group g's count: g * from
+        if (rows16) {
+            auto join = [&](K b, K s) {
+                const K low = b < best ? b : best, most = s > second ? s : second;
+                best = b > best ? b : best;
+                second = low > most ? low : most;
+            };
+            if (lanes > 1) join(dpp_take_k<0xB1>(best), dpp_take_k<0xB1>(second));
+            if (lanes > 2) join(dpp_take_k<0x4E>(best), dpp_take_k<0x4E>(second));
+            if (lanes > 4) join(dpp_take_k<0x141>(best), dpp_take_k<0x141>(second));
+            if (lanes > 8) join(dpp_take_k<0x140>(best), dpp_take_k<0x140>(second));
+            from = lanes;
+        } else {
+            if (whole) {
+                keys[2 * lane] = best;
+                keys[2 * lane + 1] = second;
+            } else {
+#pragma unroll
+                for (int i = 0; i < V; i++) keys[e0 + i] = counts(i);
             }
-        if (two && second > none) best += second;
-        int before = 0;                // groups that come before this one
+            __builtin_amdgcn_wave_barrier();
+            best = second = (K)kNone;
+            if (lane < p.groups) {
+                const K* at = keys + lane * (whole ? 2 * lanes : per);
+                const int n = whole ? 2 * lanes : per;
+#pragma unroll 4
+                for (int i = 0; i < n; i++) take(at[i]);
+            }
+        }
+        if (two && second > (K)kNone) best += second;
+        int before = 0;                                   // groups that come before lane g's; lane g: group g from here on
+        K mine_g = (K)kNone;
         for (int g = 0; g < p.groups; g++) {
-            const double v = read_lane64(best, g);
-            before += v > best || (v == best && g < lane);
+            const K v = read_lane_k(best, g * from);
+            if (lane == g) mine_g = v;
+        }
+        for (int g = 0; g < p.groups; g++) {
+            const K v = read_lane_k(best, g * from);
+            before += v > mine_g || (v == mine_g && g < lane);
         }
         const unsigned long long kept = __ballot(lane < p.groups && before < p.kept);
+        if (whole) {
+            const bool in = (kept >> (lane / lanes & 63)) & 1ull;
 #pragma unroll
-        for (int i = 0; i < V; i++) {
-            const int e = lane + 64 * i;
-            if (e < p.experts && !((kept >> (e / per)) & 1ull)) key[i] = none;
+            for (int i = 0; i < V; i++) key[i] = in ? key[i] : (K)kNone;
+        } else {
+#pragma unroll
+            for (int i = 0; i < V; i++) key[i] = (kept >> ((e0 + i) / per & 63)) & 1ull ? key[i] : (K)kNone;
         }
     }
-    int mine = -1;
-    double weight = 0., sum = 0.;
-    for (int t = 0; t < p.k; t++) {
-        double best = key[0];
+    // the lane's experts, best first, equal ones in their order
+    int of[V];
 #pragma unroll
-        for (int i = 1; i < V; i++) best = dmax(best, key[i]);
-        best = wave_all64(best, dmax);
-        if (!(best > none)) break;
-        bool found = false;
+    for (int i = 0; i < V; i++) of[i] = e0 + i;
 #pragma unroll
-        for (int i = 0; i < V; i++) {
-            const unsigned long long at = __ballot(!found && key[i] == best);
-            if (at) {
-                const int l = __builtin_ctzll(at);
-                const double w = read_lane64(pr[i], l);
-                if (lane == t) { mine = l + 64 * i; weight = w; }
-                if (lane == l) key[i] = none;
-                sum += w;
-                found = true;
+    for (int j = 1; j < V; j++)
+#pragma unroll
+        for (int i = 0; i + j < V; i++)                   // neighbours only: what is equal keeps its order
+            if (key[i + 1] > key[i]) {
+                const K k = key[i];
+                key[i] = key[i + 1];
+                key[i + 1] = k;
+                const int o = of[i];
+                of[i] = of[i + 1];
+                of[i + 1] = o;
             }
+    int mine = -1;
+    for (int t = 0; t < p.k; t++) {
+        const float head = (float)key[0], best = wave_max(head);
+        if (!(best > kNone)) break;
+        unsigned long long at = __ballot(head == best);
+        if (HIGH && (at & (at - 1))) {                    // equal in fp32: compared in fp64
+            double all = (double)kNone;
+            for (unsigned long long left = at; left; left &= left - 1) all = __builtin_fmax(all, read_lane64(key[0], __builtin_ctzll(left)));
+            at &= __ballot(key[0] == all);
+        }
+        const int l = __builtin_ctzll(at), e = __builtin_amdgcn_readlane(of[0], l);
+        if (lane == t) mine = e;
+        if (lane == l) {
+#pragma unroll
+            for (int i = 0; i + 1 < V; i++) { key[i] = key[i + 1]; of[i] = of[i + 1]; }
+            key[V - 1] = (K)kNone;
         }
     }
-    if (p.flags & 2) weight = sum > 0. ? weight / sum : 0.;
-    if (live && lane < p.k) {
-        Routed q;
-        q.expert = mine;
-        q.weight = (float)(weight * (double)p.factor);
-        ((Routed*)p.out)[(long long)row * p.k + lane] = q;
+    // the weights in fp64: a few lanes' one value each
+    double weight = 0.;
+    if (mine >= 0) {
+        double score[1] = {(double)__builtin_fminf(load_elem(sr + mine), 3.40282347e38f)};
+        scores_p(sigmoid, (double)top, score);
+        weight = score[0] * over;
     }
+    if (p.flags & 2) {
+        const double all = wave_sum64(weight);
+        weight = all > 0. ? weight / all : 0.;
+    }
+    Routed q;
+    q.expert = mine;
+    q.weight = (float)(weight * (double)p.factor);
+    if (lane < p.k) ((Routed*)p.out)[(long long)row * p.k + lane] = q;
 }
 
 // ---- PG_EXPERT_GEMV: the slots in the order of their experts ---------------------------------------------------
@@ -951,9 +1102,9 @@ __global__ __launch_bounds__(WR * WJ * 64, 2) void k_product_tile(ExpertArgs p) 
     else emit((bf16_t*)p.out);
 }
 
-template <typename T> const void* route_kernel(int experts) {
-    return experts <= 64 ? PG_FN(k_route<T, 1>) : experts <= 128 ? PG_FN(k_route<T, 2>) : experts <= 256 ? PG_FN(k_route<T, 4>) : experts <= 512 ? PG_FN(k_route<T, 8>)
-                         : PG_FN(k_route<T, 16>);
+template <typename T, bool HIGH> const void* route_kernel(long long experts) {
+    return experts <= 64 ? PG_FN(k_route<T, 1, HIGH>) : experts <= 128 ? PG_FN(k_route<T, 2, HIGH>) : experts <= 256 ? PG_FN(k_route<T, 4, HIGH>)
+         : experts <= 512 ? PG_FN(k_route<T, 8, HIGH>) : PG_FN(k_route<T, 16, HIGH>);
 }
 
 struct TileKernel {
@@ -964,10 +1115,10 @@ struct TileKernel {
 };
 #define PG_TILE(F, RM, JN, WR, WJ, S, FROM) {F, PG_FN(k_product_tile<F, false, RM, JN, WR, WJ, S>), PG_FN(k_product_tile<F, true, RM, JN, WR, WJ, S>), RM * 16 * WR, JN * 16 * WJ, WR * WJ * 64, FROM}
 const TileKernel kTileKernels[] = {
-    PG_TILE(kW8H8, 4, 8, 4, 2, 2, 128), PG_TILE(kW8H8, 2, 4, 4, 2, 4, 128),
-    PG_TILE(kW8H16, 4, 4, 2, 4, 2, 128), PG_TILE(kW8H16, 2, 4, 4, 2, 3, 128),
-    PG_TILE(kW16H16, 4, 8, 4, 2, 2, 128), PG_TILE(kW16H16, 2, 4, 4, 2, 4, 128),
-    PG_TILE(kW8H8Wide, 4, 4, 2, 4, 3, 128), PG_TILE(kW8H8Wide, 2, 4, 4, 2, 4, 128),
+    PG_TILE(kW8H8, 4, 8, 4, 2, 2, 128), PG_TILE(kW8H8, 2, 4, 4, 2, 4, 256),
+    PG_TILE(kW8H16, 4, 4, 2, 4, 2, 128), PG_TILE(kW8H16, 2, 4, 4, 2, 3, 256),
+    PG_TILE(kW16H16, 4, 8, 4, 2, 2, 128), PG_TILE(kW16H16, 2, 4, 4, 2, 4, 256),
+    PG_TILE(kW8H8Wide, 4, 4, 2, 4, 3, 128), PG_TILE(kW8H8Wide, 2, 4, 4, 2, 4, 256),
 };
 
 struct RowsKernel {
@@ -1012,7 +1163,7 @@ bool plan_experts(int op, int dtype, const Shape& s, Launch* out, Launch* pre) {
         return true;
     }
     case kRoute:
-        out->fn = f32 ? route_kernel<float>((int)s.cols) : route_kernel<bf16_t>((int)s.cols);
+        out->fn = s.high ? (f32 ? route_kernel<float, true>(s.cols) : route_kernel<bf16_t, true>(s.cols)) : f32 ? route_kernel<float, false>(s.cols) : route_kernel<bf16_t, false>(s.cols);
         out->arg_bytes = sizeof(RouteArgs);
         out->grid = dim3(blocks_for(s.rows, kBlock / 64));
         return true;
@@ -1048,7 +1199,7 @@ bool plan_experts(int op, int dtype, const Shape& s, Launch* out, Launch* pre) {
             out->fn = routed ? fit->routed : fit->plain;
             out->block = dim3(fit->threads);
         } else {
-            const long long each = routed ? (slots + std::min(slots, s.inner) - 1) / std::min(slots, s.inner) : slots;      // slots of an expert, about
+            const long long each = routed ? (3 * slots + 2 * std::min(slots, s.inner) - 1) / (2 * std::min(slots, s.inner)) : slots;      // slots of an expert: half as many again as the mean
             // the smallest tile that holds an expert's rows, up to 64 of them, with as many outputs as leave kRowsFrom workgroups
             const RowsKernel* k = kRowsKernels;
             while (k->form != form || (s.cols >= 8 && each > k->rows && k->rows < 64)) k++;

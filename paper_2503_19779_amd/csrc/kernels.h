@@ -296,6 +296,7 @@ inline void settle_weights(Launch* l, long long chain_weight_bytes) {
 struct Shape {
     long long n = 0, m = 0, rows = 1, cols = 0, inner = 0;
     int in_dtype[2] = {kBF16, kBF16};       // kGemvF8, kExpertGemv: of W and h
+    bool high = false;                      // kRoute: experts are compared by p, not by their scores
 };
 
 // Kernel instantiation and launch shape for (op, dtype, mask of indirected operands, shape).  The
