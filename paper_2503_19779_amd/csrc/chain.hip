@@ -1256,13 +1256,35 @@ std::vector<Dispatch> segment_dispatches(pg_chain* c, Segment& sg, int kind, int
         return a;
     };
     int n_carry = 0;                      // runs with a carry so far: two places for what they set aside, in turn
+    // The sorted slots that an earlier kernel of the segment left: products that go by the same routed slots, in tiles of one size, sort them once
+    std::vector<int> sorted;
+    auto sorted_before = [&](int ki) -> int {
+        const pg_kernel_desc& d = c->k[ki];
+        for (int q : sorted) {
+            const pg_kernel_desc& e = c->k[q];
+            if (e.in[2].kind != d.in[2].kind || e.in[2].index != d.in[2].index || e.rows != d.rows || e.m != d.m || e.inner != d.inner ||
+                c->rec[q].direct.tile != c->rec[ki].direct.tile) continue;
+            bool same = true;                         // nothing has written the slots since
+            for (int i = q; i < ki; i++) same = same && !(d.in[2].kind == PG_REF_INT && c->k[i].out.index == d.in[2].index);
+            if (same) return q;
+        }
+        return -1;
+    };
     for (auto& grp : sg.groups) {
         const bool* const store = every ? grp.store_every : grp.store;
         if (!c->merge || grp.k1 - grp.k0 < 2 || (every && grp.carry)) {
             for (int i = grp.k0; i < grp.k1; i++) {
                 KernelRec& r = c->rec[i];
-                const ArgBlock a = versioned(i, nullptr);
-                if (r.pre.fn) emit(r.pre, &a);
+                ArgBlock a = versioned(i, nullptr);
+                if (r.pre.fn) {
+                    const int by = c->merge ? sorted_before(i) : -1;
+                    if (by >= 0) {
+                        a.expert.sorted = c->rec[by].a_copy.expert.sorted;
+                    } else {
+                        emit(r.pre, &a);
+                        sorted.push_back(i);
+                    }
+                }
                 emit(kind == kGraphCopy ? r.direct : r.indirect, &a);
             }
             continue;
