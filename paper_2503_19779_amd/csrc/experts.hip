@@ -443,36 +443,46 @@ __device__ __forceinline__ SortedTile* sorted_tiles(void* area) { return (Sorted
 __device__ __forceinline__ int* sorted_order(void* area, int tiles) { return (int*)(sorted_tiles(area) + tiles); }
 
 // One workgroup: a slot's place among its expert's is what a count in LDS says when it is counted, and from the counts follow the places of the
-// experts.  Slots of an expert come in no fixed order, and a product's rows do not depend on it: each is a row of its own in a tile.  Whole
-// tiles come first, so that the small ones fill what is left of the chip at the end.  Bucket `experts` takes the empty slots.
+// experts.  Counts are kept in kCopies for neighbouring lanes to add to (lanes of a wave that add to one place wait for each other: 32768 slots of 64
+// experts 14 us with one).  Slots of an expert come in no fixed order, and a product's rows do not depend on it: each is a row of its own in a tile.
+// Whole tiles come first, so that the small ones fill what is left of the chip at the end.  Bucket `experts` takes the empty slots.
 __global__ __launch_bounds__(kSortThreads) void k_sort_slots(ExpertArgs p) {
-    __shared__ int cnt[kSortMostExperts + 1];
+    constexpr int kCopies = 8;
+    __shared__ int cnt[kCopies][kSortMostExperts + 1];
     __shared__ int sums[3][kSortThreads / 64];
-    __shared__ int ordered[kSortThreads * kSortHeld];
+    __shared__ unsigned short ordered[kSortThreads * kSortHeld];
     const Routed* r = operand<Routed>(p.r, p.slots, 2);
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, buckets = p.experts + 1;
     const int slots = p.rows * p.k;
     const bool few = slots <= kSortThreads * kSortHeld;      // slots and places stay in registers
+    int* const mine = cnt[lane % kCopies];
     auto bucket = [&](int e) { return (unsigned)e < (unsigned)p.experts ? e : p.experts; };
-    for (int i = tid; i < buckets; i += kSortThreads) cnt[i] = 0;
+    for (int c = 0; c < kCopies; c++)
+        for (int i = tid; i < buckets; i += kSortThreads) cnt[c][i] = 0;
+    // two neighbouring slots a load: slots (i / 2 * kSortThreads + tid) * 2 + i % 2
     int id[kSortHeld], place[kSortHeld];
+    auto slot = [&](int i) { return (i / 2 * kSortThreads + tid) * 2 + i % 2; };
     if (few) {
 #pragma unroll
-        for (int i = 0; i < kSortHeld; i++) {
-            const int s = i * kSortThreads + tid;
-            id[i] = s < slots ? r[s].expert : -1;
+        for (int i = 0; i < kSortHeld; i += 2) {
+            const int s = slot(i);
+            v4u v = {0u, 0u, 0u, 0u};
+            if (s + 1 < slots) v = *(const v4u_any PG_GLOBAL*)(uintptr_t)(r + s);
+            else if (s < slots) v.x = (unsigned)r[s].expert;
+            id[i] = (int)v.x;
+            id[i + 1] = (int)v.z;
         }
     }
     __syncthreads();
     if (few) {
 #pragma unroll
         for (int i = 0; i < kSortHeld; i++)
-            if (i * kSortThreads + tid < slots) {
+            if (slot(i) < slots) {
                 id[i] = bucket(id[i]);
-                place[i] = atomicAdd(&cnt[id[i]], 1);
+                place[i] = atomicAdd(&mine[id[i]], 1);
             }
     } else {
-        for (int s = tid; s < slots; s += kSortThreads) atomicAdd(&cnt[bucket(r[s].expert)], 1);
+        for (int s = tid; s < slots; s += kSortThreads) atomicAdd(&mine[bucket(r[s].expert)], 1);
     }
     __syncthreads();
     // in front of each bucket: slots, whole tiles, others.  A thread takes two neighbouring buckets (1025 of 1024 threads).
@@ -480,7 +490,10 @@ __global__ __launch_bounds__(kSortThreads) void k_sort_slots(ExpertArgs p) {
 #pragma unroll
     for (int q = 0; q < 2; q++) {
         const int b = tid * 2 + q;
-        c[q] = b < buckets ? cnt[b] : 0;
+        c[q] = 0;
+        if (b < buckets)
+#pragma unroll
+            for (int u = 0; u < kCopies; u++) c[q] += cnt[u][b];
         v[0] += c[q];
         v[1] += c[q] / p.tile;
         v[2] += c[q] % p.tile != 0;
@@ -510,7 +523,13 @@ __global__ __launch_bounds__(kSortThreads) void k_sort_slots(ExpertArgs p) {
         const int first = before[0], expert = b < p.experts ? b : -1, n = c[q] / p.tile;
         for (int i = 0; i < n; i++) tiles[before[1]++] = SortedTile{expert, first + i * p.tile, first + (i + 1) * p.tile, 0};
         if (c[q] % p.tile) tiles[whole + before[2]++] = SortedTile{expert, first + n * p.tile, first + c[q], 0};
-        cnt[b] = first;
+        int at = first;
+#pragma unroll
+        for (int u = 0; u < kCopies; u++) {
+            const int n_u = cnt[u][b];
+            cnt[u][b] = at;
+            at += n_u;
+        }
         before[0] += c[q];
     }
     if (tid == 0) ((SortedSlots*)p.sorted)->n_tiles = all;
@@ -519,11 +538,11 @@ __global__ __launch_bounds__(kSortThreads) void k_sort_slots(ExpertArgs p) {
     if (few) {                       // (by way of LDS: 64 scattered stores of a wave take 64 lines' time)
 #pragma unroll
         for (int i = 0; i < kSortHeld; i++)
-            if (i * kSortThreads + tid < slots) ordered[cnt[id[i]] + place[i]] = i * kSortThreads + tid;
+            if (slot(i) < slots) ordered[mine[id[i]] + place[i]] = (unsigned short)slot(i);
         __syncthreads();
         for (int s = tid; s < slots; s += kSortThreads) order[s] = ordered[s];
     } else {
-        for (int s = tid; s < slots; s += kSortThreads) order[atomicAdd(&cnt[bucket(r[s].expert)], 1)] = s;
+        for (int s = tid; s < slots; s += kSortThreads) order[atomicAdd(&mine[bucket(r[s].expert)], 1)] = s;
     }
 }
 
