@@ -595,9 +595,9 @@ struct TileOf { int expert, used; int begin; unsigned long long members; };
 template <int TILE>
 __device__ __forceinline__ TileOf routed_tile(const ExpertArgs& p, int t) {
     if (p.sorted) {
-        if (t >= ((const SortedSlots*)p.sorted)->n_tiles) return TileOf{-2, 0, 0, 0};
-        const SortedTile st = sorted_tiles(p.sorted)[t];
-        return TileOf{st.expert, st.end - st.begin, st.begin, 0};
+        const int n = ((const SortedSlots*)p.sorted)->n_tiles;
+        const SortedTile st = sorted_tiles(p.sorted)[t < p.tiles ? t : p.tiles - 1];       // (asked for beside the number of tiles, not behind it)
+        return t < n ? TileOf{st.expert, st.end - st.begin, st.begin, 0} : TileOf{-2, 0, 0, 0};
     }
     const Routed* r = operand<Routed>(p.r, p.slots, 2);
     const int slots = p.rows * p.k, lane = threadIdx.x & 63;
@@ -687,7 +687,7 @@ template <int N> __device__ __forceinline__ void wait_loads() { asm volatile("s_
 // until the partial sums meet.  Loads go by whole lines of eight rows, straight into LDS: as fragments in registers, neighbouring lanes took
 // 16 bytes of a row each, and a load the time of 64 lines (64 rows of 4096 columns 16 us for any number of outputs).
 template <Form FORM, bool ROUTED, int MT, int JT, int S, int NW>
-__global__ __launch_bounds__(NW * 64, (S * NW * ((FORM == kW8H16 ? 2 : 1) * MT + JT) * 2048 <= 76 * 1024 ? 2 : 1) * NW / 4) void k_product(ExpertArgs p) {
+__global__ __launch_bounds__(NW * 64, (150 * 1024 / (S * NW * ((FORM == kW8H16 ? 2 : 1) * MT + JT) * 2048) > 1 ? 2 : 1) * NW / 4) void k_product(ExpertArgs p) {
     constexpr bool W8 = FORM != kW16H16, H8 = FORM == kW8H8 || FORM == kW8H8Wide;
     constexpr int TILE = 16 * MT, OUTS = 16 * JT, kStep = W8 ? 128 : 64;
     constexpr int HS = W8 && !H8 ? 2 : 1;                     // pieces of 128 bytes that a row of h has of a step
@@ -735,55 +735,77 @@ __global__ __launch_bounds__(NW * 64, (S * NW * ((FORM == kW8H16 ? 2 : 1) * MT +
         const int turn = (int)((unsigned)(j0 / OUTS >> 3) * NW % (unsigned)nk), mine_n = (nk - wave + NW - 1) / NW;
         auto step = [&](int b) { const int k = wave + NW * b + turn; return k < nk ? k : k - nk; };
         // way: 0 straight into LDS; 1 by way of registers; 2 the same, rows shorter than 16 bytes
-        auto bf16_piece = [&](auto way, const unsigned char* row, int k, int more, char* dst) {
+        constexpr int kRegs = (W8 ? 0 : QW) + (H8 ? 0 : QH);
+        auto bf16_piece = [&](auto way, const unsigned char* row, int k, int more, char* dst, v4u* held) {
             constexpr int kWay = decltype(way)::value;
             const int c = k * kStep + more + piece * 8;
             if constexpr (kWay == 0) direct_to_lds((k + 1) * kStep <= p.cols || c < p.cols ? row + 2ll * c : (const unsigned char*)kZeros, dst);
-            else *(v4u*)(dst + lane * 16) = kWay == 1 ? row8_shifted((const bf16_t*)row, c, p.cols) : row8_short((const bf16_t*)row, c, p.cols);
+            else *held = kWay == 1 ? row8_shifted((const bf16_t*)row, c, p.cols) : row8_short((const bf16_t*)row, c, p.cols);
         };
-        auto issue_weights = [&](auto way, int b, char* to) {
+        auto issue_weights = [&](auto way, int b, char* to, v4u* held) {
             const int k = step(b);
 #pragma unroll
             for (int q = 0; q < QW; q++) {
                 if constexpr (W8) direct_to_lds(wp[q] + (long long)k * 128 + piece * 16, to + kHBytes + q * 1024);
-                else bf16_piece(way, wp[q], k, 0, to + kHBytes + q * 1024);
+                else bf16_piece(way, wp[q], k, 0, to + kHBytes + q * 1024, held + q);
             }
         };
-        auto issue_rows = [&](auto way, int b, char* to) {
+        auto issue_rows = [&](auto way, int b, char* to, v4u* held) {
             const int k = step(b);
             if constexpr (H8) word_to_lds(hs + (k & ~3), to + kHBytes + QW * 1024);
 #pragma unroll
             for (int q = 0; q < QH; q++) {
                 if constexpr (H8) direct_to_lds(hp[q] + (long long)k * 128 + piece * 16, to + q * 1024);
-                else bf16_piece(way, hp[q % (MT * 2)], k, q / (MT * 2) * 64, to + q * 1024);
+                else bf16_piece(way, hp[q % (MT * 2)], k, q / (MT * 2) * 64, to + q * 1024, held + (W8 ? 0 : QW) + q);
+            }
+        };
+        auto put = [&](char* to, const v4u* held) {            // what came through registers
+#pragma unroll
+            for (int q = 0; q < kRegs; q++) {
+                const int at = W8 ? q : q < QW ? QH + q : q - QW;          // (weights first)
+                *(v4u*)(to + at * 1024 + lane * 16) = held[q];
             }
         };
         float scale64 = 0.f;                                   // lane l: the scale of the wave's step l of 64
         auto load_scales = [&](int b) { if (W8) scale64 = *(const float PG_GLOBAL*)(uintptr_t)(scales + step(b + lane < mine_n ? b + lane : mine_n - 1)); };
         auto stream = [&](auto way) {
             constexpr bool kDirect = decltype(way)::value == 0;
-            constexpr int kAhead = kDirect ? S : 1;
+            // Steps on their way: a ring of S in LDS; or in registers, as many as they have room for, and 8-bit weights beside them in the ring's places
+            constexpr int kAhead = kDirect ? S : kRegs <= 10 && S >= 2 ? 2 : 1;
+            v4u held[kDirect ? 1 : kAhead][kRegs ? kRegs : 1];
             if (mine_n > 0) {
                 load_scales(0);
 #pragma unroll
-                for (int b = 0; b < kAhead; b++) if (b < mine_n) issue_weights(way, b, mine + b * kStage);
+                for (int b = 0; b < kAhead; b++) if (b < mine_n) issue_weights(way, b, mine + b * kStage, held[kDirect ? 0 : b]);
             }
             if constexpr (ROUTED) tile_slots<TILE>(p, tile, list);          // (the weights are on their way meanwhile)
 #pragma unroll
             for (int q = 0; q < MT * 2; q++) hp[q] = h + hrow(q * 8 + (lane >> 3)) * hpitch;
             if constexpr (H8) hs = h + hrows * kp + hrow(lane % TILE) * nb4;
 #pragma unroll
-            for (int b = 0; b < kAhead; b++) if (b < mine_n) issue_rows(way, b, mine + b * kStage);
+            for (int b = 0; b < kAhead; b++) if (b < mine_n) issue_rows(way, b, mine + b * kStage, held[kDirect ? 0 : b]);
             asm volatile("" : "+v"(scale64));                  // (waits for the scales here, not at each use for whatever was loaded behind them)
             int at = 0;
 #pragma unroll 1
-            for (int b = 0; b < mine_n; b++) {
+            for (int b0 = 0; b0 < mine_n; b0 += kDirect ? 1 : kAhead)
+#pragma unroll
+            for (int u = 0; u < (kDirect ? 1 : kAhead); u++) {
+                const int b = b0 + u;
+                if (!kDirect && b >= mine_n) break;
                 if (W8 && b && (b & 63) == 0) {
                     load_scales(b);
                     asm volatile("" : "+v"(scale64));
                 }
-                if (kAhead > 1 && b && b + kAhead <= mine_n) wait_loads<(kAhead - 1) * kLoads>();      // (at first rows come behind all steps' weights)
-                else wait_loads<0>();
+                if constexpr (kDirect) {
+                    if (kAhead > 1 && b && b + kAhead <= mine_n) wait_loads<(kAhead - 1) * kLoads>();      // (at first rows come behind all steps' weights)
+                    else wait_loads<0>();
+                } else {
+                    put(mine + at, held[u]);                   // (waits for this step's registers; 8-bit weights came before them)
+                    if constexpr (W8) {
+                        if (b + 1 < mine_n && kAhead > 1) wait_loads<QW + kRegs>();
+                        else wait_loads<0>();
+                    }
+                }
                 const unsigned now = mine0 + (unsigned)at;
                 unsigned exps[MT];
                 if constexpr (H8) lds_bytes<MT>(now + kHBytes + QW * 1024 + l16 * 4 + (step(b) & 3), exps);
@@ -792,10 +814,10 @@ __global__ __launch_bounds__(NW * 64, (S * NW * ((FORM == kW8H16 ? 2 : 1) * MT +
                 for (int q = 0; q < HS; q++) lds_frags<MT>(now + q * MT * 2048 + g0, now + q * MT * 2048 + g1, hf[q]);
                 lds_frags<JT>(now + kHBytes + f0, now + kHBytes + f1, wf);
                 if (b + kAhead < mine_n) {                     // (what was there has been read)
-                    issue_weights(way, b + kAhead, mine + at);
-                    issue_rows(way, b + kAhead, mine + at);
+                    issue_weights(way, b + kAhead, mine + at, held[kDirect ? 0 : u]);
+                    issue_rows(way, b + kAhead, mine + at, held[kDirect ? 0 : u]);
                 }
-                at = kAhead == 1 || at + kStage == S * kStage ? 0 : at + kStage;
+                at = at + kStage == (kDirect ? S : kAhead) * kStage ? 0 : at + kStage;
                 const float s = W8 ? __int_as_float(__builtin_amdgcn_readlane(__float_as_int(scale64), b & 63)) : 1.f;
 #pragma unroll
                 for (int j = 0; j < JT; j++) {
@@ -1134,10 +1156,10 @@ struct TileKernel {
 };
 #define PG_TILE(F, RM, JN, WR, WJ, S, FROM) {F, PG_FN(k_product_tile<F, false, RM, JN, WR, WJ, S>), PG_FN(k_product_tile<F, true, RM, JN, WR, WJ, S>), RM * 16 * WR, JN * 16 * WJ, WR * WJ * 64, FROM}
 const TileKernel kTileKernels[] = {
-    PG_TILE(kW8H8, 4, 8, 4, 2, 2, 128), PG_TILE(kW8H8, 2, 4, 4, 2, 4, 256),
+    PG_TILE(kW8H8, 4, 8, 4, 2, 2, 128), PG_TILE(kW8H8, 2, 4, 4, 2, 4, 128),
     PG_TILE(kW8H16, 4, 4, 2, 4, 2, 128), PG_TILE(kW8H16, 2, 4, 4, 2, 3, 256),
-    PG_TILE(kW16H16, 4, 8, 4, 2, 2, 128), PG_TILE(kW16H16, 2, 4, 4, 2, 4, 256),
-    PG_TILE(kW8H8Wide, 4, 4, 2, 4, 3, 128), PG_TILE(kW8H8Wide, 2, 4, 4, 2, 4, 256),
+    PG_TILE(kW16H16, 4, 8, 4, 2, 2, 128), PG_TILE(kW16H16, 2, 4, 4, 2, 4, 128),
+    PG_TILE(kW8H8Wide, 4, 4, 2, 4, 3, 128), PG_TILE(kW8H8Wide, 2, 4, 4, 2, 4, 128),
 };
 
 struct RowsKernel {
@@ -1148,10 +1170,10 @@ struct RowsKernel {
 };
 #define PG_ROWS(F, MT, JT, S, NW) {F, PG_FN(k_product<F, false, MT, JT, S, NW>), PG_FN(k_product<F, true, MT, JT, S, NW>), 16 * MT, 16 * JT, NW * 64}
 const RowsKernel kRowsKernels[] = {
-    PG_ROWS(kW16H16, 1, 1, 4, 4), PG_ROWS(kW16H16, 1, 2, 3, 4), PG_ROWS(kW16H16, 1, 4, 3, 4), PG_ROWS(kW16H16, 2, 1, 3, 4), PG_ROWS(kW16H16, 2, 2, 2, 4), PG_ROWS(kW16H16, 2, 4, 3, 4), PG_ROWS(kW16H16, 4, 1, 3, 4), PG_ROWS(kW16H16, 4, 2, 3, 4), PG_ROWS(kW16H16, 4, 4, 2, 4),
-    PG_ROWS(kW8H16, 1, 1, 3, 4), PG_ROWS(kW8H16, 1, 2, 2, 4), PG_ROWS(kW8H16, 1, 4, 3, 4), PG_ROWS(kW8H16, 2, 1, 3, 4), PG_ROWS(kW8H16, 2, 2, 3, 4), PG_ROWS(kW8H16, 2, 4, 2, 4), PG_ROWS(kW8H16, 4, 1, 2, 4), PG_ROWS(kW8H16, 4, 2, 1, 4), PG_ROWS(kW8H16, 4, 4, 1, 4),
-    PG_ROWS(kW8H8, 1, 1, 4, 4), PG_ROWS(kW8H8, 1, 2, 3, 4), PG_ROWS(kW8H8, 1, 4, 3, 4), PG_ROWS(kW8H8, 2, 1, 3, 4), PG_ROWS(kW8H8, 2, 2, 2, 4), PG_ROWS(kW8H8, 2, 4, 3, 4), PG_ROWS(kW8H8, 4, 1, 3, 4), PG_ROWS(kW8H8, 4, 2, 3, 4), PG_ROWS(kW8H8, 4, 4, 2, 4),
-    PG_ROWS(kW8H8Wide, 1, 1, 4, 4), PG_ROWS(kW8H8Wide, 1, 2, 3, 4), PG_ROWS(kW8H8Wide, 1, 4, 3, 4), PG_ROWS(kW8H8Wide, 2, 1, 3, 4), PG_ROWS(kW8H8Wide, 2, 2, 2, 4), PG_ROWS(kW8H8Wide, 2, 4, 3, 4), PG_ROWS(kW8H8Wide, 4, 1, 3, 4), PG_ROWS(kW8H8Wide, 4, 2, 3, 4), PG_ROWS(kW8H8Wide, 4, 4, 2, 4),
+    PG_ROWS(kW16H16, 1, 1, 4, 4), PG_ROWS(kW16H16, 1, 2, 2, 4), PG_ROWS(kW16H16, 1, 4, 1, 4), PG_ROWS(kW16H16, 2, 1, 2, 4), PG_ROWS(kW16H16, 2, 2, 2, 4), PG_ROWS(kW16H16, 2, 4, 1, 4), PG_ROWS(kW16H16, 4, 1, 1, 4), PG_ROWS(kW16H16, 4, 2, 1, 4), PG_ROWS(kW16H16, 4, 4, 1, 4),
+    PG_ROWS(kW8H16, 1, 1, 3, 4), PG_ROWS(kW8H16, 1, 2, 2, 4), PG_ROWS(kW8H16, 1, 4, 1, 4), PG_ROWS(kW8H16, 2, 1, 1, 4), PG_ROWS(kW8H16, 2, 2, 1, 4), PG_ROWS(kW8H16, 2, 4, 1, 4),
+    PG_ROWS(kW8H8, 1, 1, 2, 4), PG_ROWS(kW8H8, 1, 2, 2, 4), PG_ROWS(kW8H8, 1, 4, 1, 4), PG_ROWS(kW8H8, 2, 1, 2, 4), PG_ROWS(kW8H8, 2, 2, 2, 4), PG_ROWS(kW8H8, 2, 4, 1, 4), PG_ROWS(kW8H8, 4, 1, 1, 4), PG_ROWS(kW8H8, 4, 2, 1, 4), PG_ROWS(kW8H8, 4, 4, 1, 4),
+    PG_ROWS(kW8H8Wide, 1, 1, 2, 4), PG_ROWS(kW8H8Wide, 1, 2, 2, 4), PG_ROWS(kW8H8Wide, 1, 4, 1, 4), PG_ROWS(kW8H8Wide, 2, 1, 2, 4), PG_ROWS(kW8H8Wide, 2, 2, 2, 4), PG_ROWS(kW8H8Wide, 2, 4, 1, 4), PG_ROWS(kW8H8Wide, 4, 1, 1, 4), PG_ROWS(kW8H8Wide, 4, 2, 1, 4), PG_ROWS(kW8H8Wide, 4, 4, 1, 4),
 };
 
 constexpr long long kRowsFrom = 256;
@@ -1221,7 +1243,8 @@ bool plan_experts(int op, int dtype, const Shape& s, Launch* out, Launch* pre) {
             const long long each = routed ? (3 * slots + 2 * std::min(slots, s.inner) - 1) / (2 * std::min(slots, s.inner)) : slots;      // slots of an expert: half as many again as the mean
             // the smallest tile that holds an expert's rows, up to 64 of them, with as many outputs as leave kRowsFrom workgroups
             const RowsKernel* k = kRowsKernels;
-            while (k->form != form || (s.cols >= 8 && each > k->rows && k->rows < 64)) k++;
+            const int most = form == kW8H16 || (form != kW16H16 && each <= 128) ? 32 : 64;
+            while (k->form != form || (s.cols >= 8 && each > k->rows && k->rows < most)) k++;
             const long long about = routed ? std::min(slots, s.inner) * ((each + k->rows - 1) / k->rows) : (slots + k->rows - 1) / k->rows;
             while (s.cols >= 8 && k->outputs < 64 && about * ((s.n + k[1].outputs - 1) / k[1].outputs) >= kRowsFrom) k++;
             if (!with(k->rows, k->outputs)) return false;
