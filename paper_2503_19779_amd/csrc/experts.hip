@@ -1152,8 +1152,14 @@ struct TileKernel {
     Form form;
     const void* plain;
     const void* routed;
-    int rows, outputs, threads, from;        // from: workgroups
+    int rows, outputs, threads, from;        // from: the fewest workgroups that a product of whole tiles has to make (see below)
 };
+// The large tiles do the most work to a byte that they load, but leave compute units idle where a product has few of them; the first of the table that
+// the rows half fill and that makes `from` workgroups is taken.  Measured (us), this kernel against the next: 4096 columns, 4096 outputs: 8-bit rows,
+// 2048 of them, 128 large workgroups 64 against 256 smaller ones 56, 4096 rows 70 against 109; 1024 rows 30 against k_product's 46, 512 rows (128
+// workgroups) 29 against 20.  Routed rows, 4 of 4 experts for 1133 rows of 768 columns, 512 outputs (144 workgroups): 20 against k_product's 26; 2 of 8
+// for 4096 of 1024 columns, 1024 outputs (128 large workgroups): 35 against 41.  So a plain product asks for kPlainFrom.
+constexpr int kPlainFrom = 192;
 #define PG_TILE(F, RM, JN, WR, WJ, S, FROM) {F, PG_FN(k_product_tile<F, false, RM, JN, WR, WJ, S>), PG_FN(k_product_tile<F, true, RM, JN, WR, WJ, S>), RM * 16 * WR, JN * 16 * WJ, WR * WJ * 64, FROM}
 const TileKernel kTileKernels[] = {
     PG_TILE(kW8H8, 4, 8, 4, 2, 2, 128), PG_TILE(kW8H8, 2, 4, 4, 2, 4, 128),
@@ -1219,7 +1225,7 @@ bool plan_experts(int op, int dtype, const Shape& s, Launch* out, Launch* pre) {
     }
     case kGemvF8: case kExpertGemv: {
         const bool routed = op == kExpertGemv, w8 = s.in_dtype[0] == kF8Weight, h8 = s.in_dtype[1] == kF8Rows;
-        const long long slots = routed ? s.rows * s.m : s.rows;
+        const long long slots = routed ? s.rows * s.m : s.rows, experts = routed ? s.inner : 1, mean = slots / experts;
         const Form form = !w8 ? kW16H16 : !h8 ? kW8H16 : f32 ? kW8H8Wide : kW8H8;
         auto with = [&](int tile, int outputs, bool in_pairs = false) {
             out->tile = tile;
@@ -1234,7 +1240,7 @@ bool plan_experts(int op, int dtype, const Shape& s, Launch* out, Launch* pre) {
         const long long pitch = w8 ? (s.cols + kScaleBlock - 1) / kScaleBlock * kScaleBlock : 2 * s.cols, hpitch = h8 ? pitch : 2 * s.cols;
         const bool fits = s.cols >= 8 && 256 * std::max(pitch, hpitch) < (1ll << 32) && (!routed || slots * hpitch < (1ll << 32));
         for (const TileKernel& k : kTileKernels)
-            if (k.form == form && fits && 2 * slots / (routed ? s.inner : 1) >= k.rows && (slots / (routed ? s.inner : 1) + k.rows - 1) / k.rows * (routed ? s.inner : 1) * ((s.n + k.outputs - 1) / k.outputs) >= k.from) { fit = &k; break; }
+            if (k.form == form && fits && 2 * mean >= k.rows && (mean + k.rows - 1) / k.rows * experts * ((s.n + k.outputs - 1) / k.outputs) >= (routed ? k.from : std::max(k.from, kPlainFrom))) { fit = &k; break; }
         if (fit) {
             if (!with(fit->rows, fit->outputs, routed)) return false;
             out->fn = routed ? fit->routed : fit->plain;
