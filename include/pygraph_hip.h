@@ -18,7 +18,7 @@
  *     pg_last_hip_error().
  *   - Pointers marked [dev] are device addresses, [host] host addresses.  The CALLER owns all
  *     device memory: external inputs, weights and one workspace blob.  The library borrows them,
- *     carves the workspace (placeholders, internal buffers, pointer table, copy job list; each
+ *     carves the workspace (placeholders, internal buffers, pointer table, copy job list, lists of sorted slots; each
  *     sub-buffer 256-byte aligned), and allocates or frees no device memory itself.  It owns only
  *     host objects (descriptors, graphs, pinned staging).
  *   - Weights and the workspace must stay alive and unmoved until pg_chain_destroy.  External
@@ -97,9 +97,12 @@ typedef enum {
  * PG_EXPERT_GEMV  in: W PG_BF16 [inner, n, cols] or PG_F8_WEIGHT of `inner` experts, h, r PG_ROUTED [rows, m]; h [rows, cols], or with
  *                 PG_EXPERT_PER_SLOT [rows, m, cols], PG_BF16 or (with 8-bit W) PG_F8_ROWS; out [rows, m, n], dtype PG_BF16 or PG_F32; m (1 to 64),
  *                 inner = experts (1 to 1024), rows * m < 2^24.  The rows of a slot whose expert is not one of 0 .. inner - 1 are zero.
+ *                 With more than 64 slots a dispatch in front lists them by expert in the workspace (also in pg_eager_static's scratch); in a
+ *                 captured segment products that go by the same slots share it.
  * PG_EXPERT_SUM   in: z [rows, m, n], r PG_ROUTED [rows, m], and optionally x [rows, n]; dtype of z, x and the output PG_F32 or PG_BF16; rows, n, m (1 to 64).
- *                 Slots are added in order, x behind them, in fp32; an empty slot's z is not read.  out may be x's buffer.
+ *                 Slots are added in order, x behind them, in fp32; an empty slot's z counts as nothing, whatever it holds.  out may be x's buffer.
  *
+ * rows, n and cols are below 2^31 - 512, and a kernel has fewer than 2^32 threads (a row of scores takes 64, for instance).
  * An internal PG_F8_ROWS buffer is read with the rows and cols it was last written with.  External 8-bit tensors and weights have exactly the size
  * of their layout; external pointers to 8-bit tensors are aligned to 16 bytes. */
 enum { PG_ROUTE_SIGMOID = 1, PG_ROUTE_RENORMALIZE = 2, PG_ROUTE_GROUP_TOP2 = 4 };
@@ -348,7 +351,8 @@ pg_status pg_set_dispatch_merge(pg_chain *chain, int32_t on);
  * unless set, 0 = always a graph.  The results are the same.  Takes effect at the next pg_capture. */
 pg_status pg_set_launched_dispatches(pg_chain *chain, int32_t most);
 /* Kernel dispatches that the graphs of one replay, or the launches in place of a graph, come to with merging on (*merged_out) and off
- * (*unmerged_out = the number of kernels).  Either output may be NULL.  Host only. */
+ * (*unmerged_out = the number of kernels); the sorting of slots in front of a PG_EXPERT_GEMV counts as part of it.  Either output may
+ * be NULL.  Host only. */
 pg_status pg_chain_graph_dispatches(const pg_chain *chain, int32_t *merged_out, int32_t *unmerged_out);
 /* Destroys the graphs and host objects, after waiting for everything queued on the device the chain
  * was captured on (a graph still running, or a copy node still reading pinned staging, must not lose

@@ -31,7 +31,8 @@ pg_status pg_time_loop_each(pg_chain *chain, int32_t mode, const uint8_t *mode_p
 /* GPU execution time of each kernel: launches kernels [k_begin, k_end) eagerly (as pg_eager_range
  * does), each with a pair of events that take the kernel's own start and end timestamps,
  * synchronises the stream, and writes k_end - k_begin durations in microseconds to dur_us_out
- * [host].  For roofline figures: time between launches is not included. */
+ * [host].  For roofline figures: time between launches is not included, nor the sorting of slots in front of a
+ * PG_EXPERT_GEMV. */
 pg_status pg_time_kernels(pg_chain *chain, const void *const *ext_dev_ptrs, int32_t k_begin, int32_t k_end,
                           void *hip_stream, float *dur_us_out);
 

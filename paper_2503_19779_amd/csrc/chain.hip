@@ -373,8 +373,10 @@ pg_status validate(const pg_kernel_desc* k, int nk, const pg_tensor_desc* ext, i
             break;
         }
         default: {
-            if (!fits_i32(d.rows) || !fits_i32(d.n)) return fail(PG_EINVAL, "kernel %d: bad rows/n", i);
-            if (d.op != PG_EXPERT_SUM && !fits_i32(plus(d.cols, pgk::kScaleBlock))) return fail(PG_EINVAL, "kernel %d: bad cols", i);
+            // (a tile, or four blocks of a row, may reach beyond the last row, output and column: their numbers have 32 bits)
+            auto fits = [](long long v) { return v > 0 && fits_i32(plus(v, 4 * pgk::kScaleBlock)); };
+            if (!fits(d.rows) || !fits(d.n)) return fail(PG_EINVAL, "kernel %d: bad rows/n", i);
+            if (d.op != PG_EXPERT_SUM && !fits(d.cols)) return fail(PG_EINVAL, "kernel %d: bad cols", i);
             const int flags = d.op == PG_ROUTE ? PG_ROUTE_SIGMOID | PG_ROUTE_RENORMALIZE | PG_ROUTE_GROUP_TOP2 : d.op == PG_EXPERT_GEMV ? PG_EXPERT_PER_SLOT : 0;
             if (d.flags & ~flags) return fail(PG_EINVAL, "kernel %d: unknown flags", i);
             if (d.op == PG_QUANTIZE && d.n != d.cols) return fail(PG_EINVAL, "kernel %d: n must equal cols", i);

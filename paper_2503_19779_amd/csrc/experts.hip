@@ -1195,7 +1195,7 @@ size_t sorted_bytes(int op, const Shape& s) {
     return sizeof(SortedSlots) + (size_t)most_tiles(slots, s.inner, kSmallestTile) * sizeof(SortedTile) + (size_t)slots * sizeof(int);
 }
 
-bool plan_experts(int op, int dtype, const Shape& s, Launch* out, Launch* pre) {
+static bool plan_kernel(int op, int dtype, const Shape& s, Launch* out, Launch* pre) {
     *out = Launch();
     *pre = Launch();
     out->block = dim3(kBlock);
@@ -1203,7 +1203,7 @@ bool plan_experts(int op, int dtype, const Shape& s, Launch* out, Launch* pre) {
     switch (op) {
     case kQuantize: {
         const long long units = s.rows * (((s.cols + kScaleBlock - 1) / kScaleBlock + 3) / 4);
-        if (units >= (1ll << 31)) return false;
+        if (units >= 1ll << 31) return false;
         out->fn = f32 ? PG_FN(k_quantize<float>) : PG_FN(k_quantize<bf16_t>);
         out->arg_bytes = sizeof(QuantizeArgs);
         out->grid = dim3(blocks_for(units, kBlock / 16));
@@ -1266,6 +1266,10 @@ bool plan_experts(int op, int dtype, const Shape& s, Launch* out, Launch* pre) {
     }
     default: return false;
     }
+}
+
+bool plan_experts(int op, int dtype, const Shape& s, Launch* out, Launch* pre) {
+    return plan_kernel(op, dtype, s, out, pre) && (unsigned long long)out->grid.x * out->block.x < 1ull << 32;       // (threads of a launch)
 }
 
 }  // namespace pgk

@@ -153,3 +153,26 @@ def test_workspace_sizes_of_unvalidated_descriptors():
             pg.Chain.host_only(s)
         except pg.PgError:
             pass
+
+
+def test_sizes_near_32_bits():
+    """Row, output and column numbers reach up to 512 beyond the last one; a launch has fewer than 2^32 threads.  At the limit: built or refused, by the
+    same rule in 64 bits."""
+    most, over = (1 << 31) - 513, (1 << 31) - 512
+    wb, rb = pg.scaled_weight_bytes, pg.scaled_rows_bytes
+
+    def one(op, ins, n, ext, out, weights=(), dtype="bf16", **f):
+        return ChainSpec("x", [KernelSpec(op, dtype, 0, ins, n, **f)], [TensorSpec(*t) for t in ext], [TensorSpec(*out)], [TensorSpec(*t) for t in weights], [0])
+
+    def products(n, cols):
+        return [one("gemv_f8", (W(0), E(0)), n, [("bf16", cols)], ("bf16", n), [("f8_weight", wb(1, n, cols))], rows=1, cols=cols),
+                one("expert_gemv", (W(0), E(0), E(1)), n, [("bf16", cols), ("routed", 1)], ("bf16", n), [("bf16", n * cols)], rows=1, cols=cols, m=1, inner=1)]
+    quantize = lambda cols: one("quantize", (E(0),), cols, [("bf16", cols)], ("f8_rows", rb(1, cols)), rows=1, cols=cols)
+    total = lambda n: one("expert_sum", (E(0), E(1)), n, [("bf16", n), ("routed", 1)], ("bf16", n), rows=1, m=1)
+    route = lambda rows: one("route", (E(0),), 1, [("bf16", rows)], ("routed", rows), rows=rows, cols=1)
+    for spec in [quantize(most), total(most), route((1 << 26) - 4)] + products(1, most) + products((1 << 24) - 16, 1):
+        pg.Chain.host_only(spec)
+    for spec in [quantize(over), total(over), route(over), route(1 << 26)] + products(1, over) + products(over, 1):
+        with pytest.raises(pg.PgError) as e:
+            pg.Chain.host_only(spec)
+        assert e.value.status == 1
