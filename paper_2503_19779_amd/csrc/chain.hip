@@ -1260,8 +1260,10 @@ std::vector<Dispatch> segment_dispatches(pg_chain* c, Segment& sg, int kind, int
     int n_carry = 0;                      // runs with a carry so far: two places for what they set aside, in turn
     // The sorted slots that an earlier kernel of the segment left: products that go by the same routed slots, in tiles of one size, sort them once
     std::vector<int> sorted;
+    // -- unless they come by a pointer that the caller gives with the replay, which may lie in a buffer that the chain writes in between.
     auto sorted_before = [&](int ki) -> int {
         const pg_kernel_desc& d = c->k[ki];
+        if (d.in[2].kind == PG_REF_EXT && kind != kGraphCopy) return -1;
         for (int q : sorted) {
             const pg_kernel_desc& e = c->k[q];
             if (e.in[2].kind != d.in[2].kind || e.in[2].index != d.in[2].index || e.rows != d.rows || e.m != d.m || e.inner != d.inner ||

@@ -42,8 +42,8 @@ class Run:
         for c in self.chains:
             for mode in ("eager", "replay_copy", "replay_indirect", "replay_update"):
                 for again in range(2):                 # graphs are replayed, with the same results
-                    [c.int_buffer(i).fill_(-1 if t.dtype in ("routed",) else 255 if t.dtype.startswith("f8") else math.nan)
-                                        for i, t in enumerate(self.spec.ints)]
+                    for i, t in enumerate(self.spec.ints):
+                        c.int_buffer(i).fill_(-1 if t.dtype == "routed" else 255 if t.dtype == "f8_rows" else math.nan)
                     torch.cuda.synchronize()
                     getattr(c, mode)(ext, self.stream)
                     self.stream.synchronize()
@@ -366,3 +366,210 @@ def test_layer_of_experts(rows, hidden, width, experts, k, eightbit):
             y, a = terms.sum(1) + xr, terms.abs().sum(1) + xr.abs()
             plain.assert_within(got[:y.numel()].view(y.shape), y, plain.sum_tolerance(y, a, k + 1, torch.bfloat16), f"kernel {n}")
     r.close()
+
+
+# ------------------------------------------------------------------ lengths, tiles and orders
+@pytest.mark.parametrize("w,h", [("bf16", "bf16"), ("f8", "bf16"), ("f8", "f8")])
+@pytest.mark.parametrize("rows,k,experts,n,cols,out", [(33, 2, 9, 40, 264, "bf16"), (30, 8, 300, 33, 136, "f32"), (9, 20, 3, 300, 520, "bf16"), (9000, 4, 5, 20, 40, "bf16"),
+                                                       (700, 60, 1024, 9, 24, "f32"), (1300, 4, 3, 520, 129, "bf16"), (4000, 1, 2, 1030, 72, "f32"), (2500, 2, 40, 700, 65, "bf16")])
+def test_expert_gemv_slots(rows, k, experts, n, cols, out, w, h):
+    """Slots on both sides of every bound of the sorting, in small and large tiles."""
+    say("expert_gemv slots", rows, k, experts, n, cols, out, w, h)
+    g = torch.Generator().manual_seed(rows + k)
+    ids = torch.randint(-1, experts, (rows, k), generator=g)
+    ids[torch.rand(rows, k, generator=g) < 0.3] = experts // 2            # one has many more than the others
+    product_case(rows + n, rows, n, cols, w, h, out, experts, k, False, False, ids)
+
+
+@pytest.mark.parametrize("out", ["bf16", "f32"])
+@pytest.mark.parametrize("h", ["bf16", "f8"])
+@pytest.mark.parametrize("rows", [9, 20, 50, 140, 333])
+@pytest.mark.parametrize("n,cols", [(50, 200), (8230, 72), (16500, 33)])
+def test_gemv_f8_outputs(n, cols, rows, h, out):
+    """Tiles of every number of rows and outputs, with a tail in both and in the columns."""
+    say("gemv_f8 outputs", rows, n, cols, h, out)
+    product_case(rows + n, rows, n, cols, "f8", h, out, odd=cols == 33)
+
+
+@pytest.mark.parametrize("out", ["bf16", "f32"])
+@pytest.mark.parametrize("h", ["bf16", "f8"])
+@pytest.mark.parametrize("rows,n,cols", [(803, 3700, 129), (3900, 3001, 65), (1500, 2500, 640), (2, 40, 40000), (40, 70, 33100), (420, 6200, 8330)])
+def test_gemv_f8_large(rows, n, cols, h, out):
+    """Large tiles, and more than 64 steps of columns, whose scales are loaded 64 at a time."""
+    say("gemv_f8 large", rows, n, cols, h, out)
+    product_case(rows + n, rows, n, cols, "f8", h, out)
+
+
+@pytest.mark.parametrize("rows", [37, 300, 1500])
+@pytest.mark.parametrize("w,h", [("bf16", "bf16"), ("f8", "bf16"), ("f8", "f8")])
+def test_a_row_stays_its_own(rows, w, h):
+    """What is infinite or no number in one row of h, or in the weights of one expert, reaches that row's slots or that expert's and no others: the
+    rest keep their bits."""
+    say("a row stays its own", rows, w, h)
+    k, experts, n, cols = 2, 4, 260, 136
+    g = torch.Generator().manual_seed(rows)
+    ids = torch.randint(0, experts, (rows, k), generator=g)
+    pairs = torch.stack([ids, torch.zeros_like(ids)], -1).to(torch.int32).contiguous()
+    hv = torch.randn(rows, cols, generator=g)
+    bad = hv.clone()
+    bad[rows // 2, 5], bad[rows - 1, 130] = math.inf, math.nan
+    wv = torch.randn(experts, n, cols, generator=g)
+    wt = wv.to(torch.bfloat16) if w == "bf16" else plain.pack_weight(wv * 0.05, g)[0]
+    if w == "bf16":
+        broken = wt.clone()
+        broken[1] = math.nan
+    else:
+        broken = wt.clone()
+        broken[n * 256:2 * n * 256] = 0x7f
+    kern = KernelSpec("expert_gemv", "bf16", 0, (Ref(WEIGHT, 0), Ref(EXT, 0), Ref(EXT, 1)), n, rows=rows, cols=cols, m=k, inner=experts)
+
+    def run(hx, wx):
+        t = hx.to(torch.bfloat16) if h == "bf16" else plain.pack_rows(hx)
+        return run_one(kern, {"specs": [("bf16" if h == "bf16" else "f8_rows", t.numel()), ("routed", rows * k)], "tensors": [t.cuda(), pairs.cuda()]}, ("bf16", rows * k * n), rows * k * n,
+                       [wx.contiguous()], ["bf16" if w == "bf16" else "f8_weight"]).view(rows, k, n).cpu()
+    clean = run(hv, wt)
+    assert bool(torch.isfinite(clean).all())
+    got = run(bad, wt)
+    other = torch.ones(rows, dtype=torch.bool)
+    other[rows // 2] = other[rows - 1] = False
+    assert torch.equal(got[other].view(torch.int16), clean[other].view(torch.int16))
+    assert not bool(torch.isfinite(got[~other]).any())
+    got = run(hv, broken)
+    assert torch.equal(got[ids != 1].view(torch.int16), clean[ids != 1].view(torch.int16))
+    assert bool(torch.isnan(got[ids == 1]).all())
+
+
+# ------------------------------------------------------------------ products that share their slots' order
+def shared_chain(rows, k, experts, n, cols, external):
+    """Two products by one list of slots, which is then written anew, and a third."""
+    E, I, W = (lambda j: Ref(EXT, j)), (lambda j: Ref(INT, j)), (lambda j: Ref(WEIGHT, j))
+    r = E(3) if external else I(0)
+    ks = [KernelSpec("route", "f32", 0, (E(0),), k, rows=rows, cols=experts),
+          KernelSpec("expert_gemv", "bf16", 1, (W(0), E(2), r), n, rows=rows, cols=cols, m=k, inner=experts),
+          KernelSpec("expert_gemv", "f32", 2, (W(0), E(2), r), n, rows=rows, cols=cols, m=k, inner=experts),
+          KernelSpec("route", "f32", 0, (E(1),), k, rows=rows, cols=experts),
+          KernelSpec("expert_gemv", "bf16", 3, (W(0), E(2), r), n, rows=rows, cols=cols, m=k, inner=experts),
+          KernelSpec("expert_gemv", "bf16", 4, (W(0), E(2), r), n, rows=rows, cols=cols, m=k, inner=experts)]
+    ext = [TensorSpec("f32", rows * experts)] * 2 + [TensorSpec("bf16", rows * cols)] + ([TensorSpec("routed", rows * k)] if external else [])
+    total = rows * k * n
+    return ChainSpec("shared", ks, ext, [TensorSpec("routed", rows * k), TensorSpec("bf16", total), TensorSpec("f32", total), TensorSpec("bf16", total), TensorSpec("bf16", total)],
+                     [TensorSpec("bf16", experts * n * cols)], [1])
+
+
+@pytest.mark.parametrize("rows,k", [(20, 2), (50, 2), (400, 3)])
+def test_products_by_the_same_slots(rows, k):
+    """The list is written again between products, and again with other inputs in the next replay: each product goes by what is there then."""
+    say("products by the same slots", rows, k)
+    experts, n, cols = 7, 136, 72
+    spec = shared_chain(rows, k, experts, n, cols, False)
+    g = torch.Generator().manual_seed(rows)
+    w = (torch.randn(experts, n, cols, generator=g) * 0.1).to(torch.bfloat16)
+    run = Run(spec, [w])
+    for again in range(2):
+        s = [torch.randn(rows, experts, generator=g) for _ in range(2)]
+        h = torch.randn(rows, cols, generator=g).to(torch.bfloat16)
+        got = run(s + [h], [rows * k] + [rows * k * n] * 4)
+        for at, scores, dtype in ((1, s[0], torch.bfloat16), (2, s[0], torch.float32), (3, s[1], torch.bfloat16), (4, s[1], torch.bfloat16)):
+            ids, _ = plain.route(scores, None, k)
+            y, a = plain.product(w.double(), h.double(), ids)
+            plain.assert_within(got[at].view(y.shape), y, plain.sum_tolerance(y, a, cols, dtype), f"product {at}")
+    run.close()
+
+
+def test_slots_in_a_buffer_of_the_chain():
+    """The external list of slots is the chain's own buffer, written between the products: read there when a product runs, except in copy form, which
+    reads it when the replay begins."""
+    rows, k, experts, n, cols = 50, 2, 7, 136, 72
+    say("slots in a buffer of the chain")
+    spec = shared_chain(rows, k, experts, n, cols, True)
+    g = torch.Generator().manual_seed(3)
+    w = (torch.randn(experts, n, cols, generator=g) * 0.1).to(torch.bfloat16)
+    s = [torch.randn(rows, experts, generator=g).cuda() for _ in range(2)]
+    h = torch.randn(rows, cols, generator=g).to(torch.bfloat16).cuda()
+    stream = torch.cuda.Stream()
+    c = pg.Chain(spec, [w.cuda()], "cuda:0")
+    torch.cuda.synchronize()
+    want = [plain.product(w.double(), h.cpu().double(), plain.route(x.cpu(), None, k)[0]) for x in s]
+    for most in (0, 6):
+        c.set_launched_dispatches(most)
+        c.capture(stream)
+        ext = s + [h, c.int_buffer(0)]
+        for mode in ("eager", "replay_indirect", "replay_update", "replay_copy", "replay_indirect"):
+            for again in range(2):
+                for i in range(1, 5):
+                    c.int_buffer(i).fill_(math.nan)
+                torch.cuda.synchronize()
+                getattr(c, mode)(ext, stream)
+                stream.synchronize()
+                for at, by in ((1, 0), (2, 0), (3, 1), (4, 1)):
+                    y, a = want[1 if mode == "replay_copy" else by]
+                    dt = torch.float32 if at == 2 else torch.bfloat16
+                    plain.assert_within(c.int_buffer(at)[:y.numel()].view(y.shape), y, plain.sum_tolerance(y, a, cols, dt), f"{mode}, product {at}")
+    c.close()
+
+
+# ------------------------------------------------------------------ other ways in
+def test_static_pass_and_other_streams():
+    """The layer in the library's own scratch, with lists of sorted slots in it; eagerly on the default device's other streams; two chains at once."""
+    say("static pass, other streams")
+    rows, hidden, width, experts, k = 40, 256, 128, 6, 2
+    spec, wts, _ = expert_layer(rows, hidden, width, experts, k, True)
+    dev = [t.cuda() for t in wts]
+    chains = [pg.Chain(spec, dev, "cuda:0") for _ in range(2)]
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    xs = [torch.randn(rows, hidden, generator=torch.Generator().manual_seed(i)).to(torch.bfloat16).cuda() for i in range(2)]
+    torch.cuda.synchronize()
+    alone = []
+    for c, x, s in zip(chains, xs, streams):
+        c.eager([x], s)
+        s.synchronize()
+        alone.append(c.int_buffer(0)[:rows * hidden].clone())
+    assert bool(torch.isfinite(alone[0]).all()) and not torch.equal(alone[0], alone[1])
+    for c, s in zip(chains, streams):
+        c.capture(s)
+    for again in range(3):
+        for c in chains:
+            c.int_buffer(0).fill_(math.nan)
+        torch.cuda.synchronize()
+        for i in range(2):                                  # both under way at once
+            chains[i].replay_indirect([xs[i]], streams[i])
+        for i in range(2):
+            chains[i].eager([xs[i]], streams[i])
+            chains[i].replay_copy([xs[i]], streams[i])
+        torch.cuda.synchronize()
+        for c, want in zip(chains, alone):
+            assert torch.equal(c.int_buffer(0)[:rows * hidden], want), again
+    out = torch.full((rows * hidden,), math.nan, dtype=torch.bfloat16, device="cuda")
+    torch.cuda.synchronize()
+    for i in range(2):
+        pg.eager_static(spec, dev, [xs[i]], 0, out, streams[i])
+        streams[i].synchronize()
+        assert torch.equal(out, alone[i])
+    for c in chains:
+        c.close()
+
+
+def test_a_segment_of_its_own():
+    """The layer in four segments, each in every mode that it has."""
+    say("segments")
+    rows, hidden, width, experts, k = 50, 128, 72, 5, 2
+    spec, wts, _ = expert_layer(rows, hidden, width, experts, k, True)
+    n = len(spec.kernels)
+    ks = [KernelSpec(**{**vars(q), "segment": i * 4 // n}) for i, q in enumerate(spec.kernels)]
+    spec = ChainSpec("segments", ks, spec.ext, spec.ints, spec.weights, spec.outputs)
+    c = pg.Chain(spec, [t.cuda() for t in wts], "cuda:0")
+    stream = torch.cuda.Stream()
+    x = [torch.randn(rows, hidden, generator=torch.Generator().manual_seed(2)).to(torch.bfloat16).cuda()]
+    torch.cuda.synchronize()
+    c.capture(stream)
+    c.eager(x, stream)
+    stream.synchronize()
+    want = c.int_buffer(0).clone()
+    for modes in ([0, 1, 0, 1], [2, 0, 1, 0], [1, 1, 1, 1], [2, 1, 0, 1]):
+        for again in range(2):
+            c.int_buffer(0).fill_(math.nan)
+            torch.cuda.synchronize()
+            c.run_selected(modes, x, stream)
+            stream.synchronize()
+            assert torch.equal(c.int_buffer(0), want), modes
+    c.close()
