@@ -1148,25 +1148,35 @@ template <typename T, bool HIGH> const void* route_kernel(long long experts) {
          : experts <= 512 ? PG_FN(k_route<T, 8, HIGH>) : PG_FN(k_route<T, 16, HIGH>);
 }
 
+constexpr long long kComputeUnits = 256;
 struct TileKernel {
     Form form;
     const void* plain;
     const void* routed;
-    int rows, outputs, threads, from;        // from: the fewest workgroups that a product of whole tiles has to make (see below)
+    int rows, outputs, threads;
+    int round, both;        // what a round of up to 256 workgroups takes, and one of up to 512 where two fit a compute unit (0: they don't)
+    long long workgroups(long long slots, long long experts, long long n) const {        // (slots that are spread evenly, and half a tile more for each expert)
+        return (experts > 1 ? (2 * slots / rows + experts) / 2 : (slots + rows - 1) / rows) * ((n + outputs - 1) / outputs);
+    }
+    long long cost(long long wgs) const {
+        const long long cap = both ? 2 * kComputeUnits : kComputeUnits, rest = wgs % cap;
+        return wgs / cap * (both ? both : round) + (!rest ? 0 : rest <= kComputeUnits ? round : both);
+    }
 };
-// The large tiles do the most work to a byte that they load, but leave compute units idle where a product has few of them; the first of the table that
-// the rows half fill and that makes `from` workgroups is taken.  Measured (us), this kernel against the next: 4096 columns, 4096 outputs: 8-bit rows,
-// 2048 of them, 128 large workgroups 64 against 256 smaller ones 56, 4096 rows 70 against 109; 1024 rows 30 against k_product's 46, 512 rows (128
-// workgroups) 29 against 20.  Routed rows, 4 of 4 experts for 1133 rows of 768 columns, 512 outputs (144 workgroups): 20 against k_product's 26; 2 of 8
-// for 4096 of 1024 columns, 1024 outputs (128 large workgroups): 35 against 41.  So a plain product asks for kPlainFrom.
-constexpr int kPlainFrom = 192;
-#define PG_TILE(F, RM, JN, WR, WJ, S, FROM) {F, PG_FN(k_product_tile<F, false, RM, JN, WR, WJ, S>), PG_FN(k_product_tile<F, true, RM, JN, WR, WJ, S>), RM * 16 * WR, JN * 16 * WJ, WR * WJ * 64, FROM}
+#define PG_TILE(F, RM, JN, WR, WJ, S, ROUND, BOTH) {F, PG_FN(k_product_tile<F, false, RM, JN, WR, WJ, S>), PG_FN(k_product_tile<F, true, RM, JN, WR, WJ, S>), RM * 16 * WR, JN * 16 * WJ, WR * WJ * 64, ROUND, BOTH}
+// The large tiles do the most work to a byte that they load, but a round of them that the chip cannot fill takes as long as a full one.  What a round
+// takes is measured, in us: 8-bit rows and bf16 beside 8-bit weights with 4096 columns, bf16 with 1024.  The cheapest of a form is taken.  4096 outputs:
+// 1024 rows 30 us (8 waves), 2048 rows 41 (4 waves, two workgroups to a compute unit; 56 with 8 waves, 64 with the large tile), 4096 rows 67 (large; 79
+// with 4 waves, 109 with 8).  With fewer workgroups of the smallest tile than kTilesFrom the rows are few, and k_product, which splits K, has more of
+// them: 512 rows (128 workgroups) 20 against 29; slots 26 against 20 (4 of 4 experts for 1133 rows of 768 columns, 512 outputs, 144 workgroups).
 const TileKernel kTileKernels[] = {
-    PG_TILE(kW8H8, 4, 8, 4, 2, 2, 128), PG_TILE(kW8H8, 2, 4, 4, 2, 4, 128),
-    PG_TILE(kW8H16, 4, 4, 2, 4, 2, 128), PG_TILE(kW8H16, 2, 4, 4, 2, 3, 256),
-    PG_TILE(kW16H16, 4, 8, 4, 2, 2, 128), PG_TILE(kW16H16, 2, 4, 4, 2, 4, 128),
-    PG_TILE(kW8H8Wide, 4, 4, 2, 4, 3, 128), PG_TILE(kW8H8Wide, 2, 4, 4, 2, 4, 128),
+    PG_TILE(kW8H8, 4, 8, 4, 2, 2, 67, 0), PG_TILE(kW8H8, 4, 4, 2, 2, 2, 32, 41), PG_TILE(kW8H8, 2, 4, 4, 2, 4, 30, 0),
+    PG_TILE(kW8H16, 4, 4, 2, 4, 2, 65, 0), PG_TILE(kW8H16, 2, 4, 4, 2, 3, 45, 0),
+    PG_TILE(kW16H16, 4, 8, 4, 2, 2, 36, 0), PG_TILE(kW16H16, 4, 4, 2, 2, 2, 20, 24), PG_TILE(kW16H16, 2, 4, 4, 2, 4, 16, 0),
+    PG_TILE(kW8H8Wide, 4, 4, 2, 2, 2, 50, 65), PG_TILE(kW8H8Wide, 2, 4, 4, 2, 4, 48, 0),
 };
+constexpr int kTilesRows = 128;        // of the smallest tile
+constexpr long long tiles_from(bool routed, bool eight, bool rows16) { return eight && rows16 ? 256 : routed ? 128 : 192; }
 
 struct RowsKernel {
     Form form;
@@ -1239,8 +1249,16 @@ static bool plan_kernel(int op, int dtype, const Shape& s, Launch* out, Launch* 
         // (their offsets within a tile, and of gathered rows within h, have 32 bits)
         const long long pitch = w8 ? (s.cols + kScaleBlock - 1) / kScaleBlock * kScaleBlock : 2 * s.cols, hpitch = h8 ? pitch : 2 * s.cols;
         const bool fits = s.cols >= 8 && 256 * std::max(pitch, hpitch) < (1ll << 32) && (!routed || slots * hpitch < (1ll << 32));
-        for (const TileKernel& k : kTileKernels)
-            if (k.form == form && fits && 2 * mean >= k.rows && (mean + k.rows - 1) / k.rows * experts * ((s.n + k.outputs - 1) / k.outputs) >= (routed ? k.from : std::max(k.from, kPlainFrom))) { fit = &k; break; }
+        if (fits && 2 * mean >= kTilesRows) {
+            long long least = 0, smallest = 0;
+            for (const TileKernel& k : kTileKernels) {
+                if (k.form != form) continue;
+                const long long wgs = k.workgroups(slots, experts, s.n), cost = k.cost(wgs);
+                if (2 * mean >= k.rows && (!fit || cost < least)) { fit = &k; least = cost; }
+                smallest = wgs;                          // (the last of a form)
+            }
+            if (smallest < tiles_from(routed, w8, !h8)) fit = nullptr;
+        }
         if (fit) {
             if (!with(fit->rows, fit->outputs, routed)) return false;
             out->fn = routed ? fit->routed : fit->plain;
