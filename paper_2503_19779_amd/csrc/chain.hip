@@ -979,7 +979,10 @@ pg_status make_records(pg_chain* c) {
             if (!pgk::plan_experts(d.op, d.dtype, sh, &r.direct, &r.pre)) return fail(PG_EINVAL, "kernel %d: no device kernel for op %d dtype %d", i, d.op, d.dtype);
             r.indirect = r.direct;
             if (d.op == PG_GEMV_F8 || d.op == PG_EXPERT_GEMV)
-                for (ArgBlock* a : {&r.a_eager, &r.a_copy, &r.a_ind}) { a->expert.tile = r.direct.tile; a->expert.tiles = r.direct.tiles; }
+                for (ArgBlock* a : {&r.a_eager, &r.a_copy, &r.a_ind}) {
+                    a->expert.tile = r.direct.tile; a->expert.tiles = r.direct.tiles;
+                    if (!r.pre.fn) a->expert.sorted = nullptr;
+                }
         } else if (!pgk::plan(d.op, d.dtype, 0, sh, &r.direct) || !pgk::plan(d.op, d.dtype, r.ind_mask, sh, &r.indirect))
             return fail(PG_EINVAL, "kernel %d: no device kernel for op %d dtype %d", i, d.op, d.dtype);
         if (r.direct.grid.x != r.indirect.grid.x || r.direct.block.x != r.indirect.block.x)

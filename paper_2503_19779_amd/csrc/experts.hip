@@ -631,6 +631,72 @@ __device__ __forceinline__ void tile_slots(const ExpertArgs& p, const TileOf& ti
     __builtin_amdgcn_wave_barrier();
 }
 
+// The i-th of its slots to lane i, the last one again where there are fewer than 64
+__device__ __forceinline__ int tile_slot(const ExpertArgs& p, const TileOf& tile) {
+    const int lane = threadIdx.x & 63;
+    if (p.sorted) return sorted_order(p.sorted, p.tiles)[tile.begin + (lane < tile.used ? lane : tile.used - 1)];
+    const unsigned long long before = (1ull << lane) - 1ull;
+    const int to = (tile.members >> lane) & 1ull ? __popcll(tile.members & before) : tile.used + __popcll(~tile.members & before);       // (a place for every lane)
+    const int slot = __builtin_amdgcn_ds_permute(to * 4, lane);
+    return lane < tile.used ? slot : __builtin_amdgcn_readlane(slot, tile.used - 1);
+}
+// The same for up to kSomeSlots, by the workgroup: the slots of each expert are counted (cnt: experts + 1 places, the last for empty slots), tiles are
+// numbered by expert, and the slots of a tile follow in their order.
+constexpr int kSomeSlots = 256;
+template <int TILE, int THREADS>
+__device__ __forceinline__ TileOf counted_tile(const ExpertArgs& p, int t, int* cnt, unsigned short* ids, int* list, int& slot) {
+    constexpr int kEach = kSomeSlots / THREADS;
+    static_assert(kEach * THREADS == kSomeSlots && TILE <= 64, "slots, lanes");
+    const Routed* r = operand<Routed>(p.r, p.slots, 2);
+    const int slots = p.rows * p.k, lane = threadIdx.x & 63, buckets = p.experts + 1;
+    int e[kEach];
+#pragma unroll
+    for (int i = 0; i < kEach; i++) {
+        const int s = i * THREADS + threadIdx.x;
+        e[i] = s < slots ? r[s].expert : 0;
+    }
+    for (int i = threadIdx.x; i < buckets; i += THREADS) cnt[i] = 0;
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < kEach; i++) {
+        const int s = i * THREADS + threadIdx.x, id = (unsigned)e[i] < (unsigned)p.experts ? e[i] : p.experts;
+        if (s >= slots) continue;
+        ids[s] = (unsigned short)id;
+        atomicAdd(&cnt[id], 1);
+    }
+    __syncthreads();
+    int expert = -2, first = 0, used = 0, base = 0;
+    for (int b0 = 0; b0 < buckets && expert == -2; b0 += 64) {       // (uniform)
+        const int c = b0 + lane < buckets ? cnt[b0 + lane] : 0, n = (c + TILE - 1) / TILE;
+        int upto = n;
+        for (int d = 1; d < 64; d <<= 1) {
+            const int a = __shfl_up(upto, d);
+            if (lane >= d) upto += a;
+        }
+        const unsigned long long beyond = __ballot(base + upto > t);
+        if (beyond) {
+            const int l = __builtin_ctzll(beyond);
+            expert = b0 + l;
+            first = (t - base - __builtin_amdgcn_readlane(upto - n, l)) * TILE;
+            used = __builtin_amdgcn_readlane(c, l) - first;
+            used = used < TILE ? used : TILE;
+        }
+        base += __builtin_amdgcn_readlane(upto, 63);
+    }
+    if (expert == -2) return TileOf{-2, 0, 0, 0};
+    int rank = -first;
+    for (int s0 = 0; s0 < slots; s0 += 64) {
+        const int id = s0 + lane < slots ? ids[s0 + lane] : -1;
+        const unsigned long long same = __ballot(id == expert);
+        const int at = rank + __popcll(same & ((1ull << lane) - 1ull));
+        if (id == expert && at >= 0 && at < used) list[at] = s0 + lane;          // (by each wave, the same)
+        rank += __popcll(same);
+    }
+    __syncthreads();                                         // (what comes next takes the counts' place)
+    slot = list[lane < used ? lane : used - 1];
+    return TileOf{expert < p.experts ? expert : -1, used, 0, 0};
+}
+
 __device__ const v4u kZeros[1] = {{0u, 0u, 0u, 0u}};
 // 16 bytes a lane from global memory into LDS, lane l's at `to` + 16 l
 __device__ __forceinline__ void direct_to_lds(const unsigned char* base /* uniform */, unsigned off, char* to /* uniform */) {
@@ -696,15 +762,19 @@ __global__ __launch_bounds__(NW * 64, (150 * 1024 / (S * NW * ((FORM == kW8H16 ?
     constexpr int kRing = NW * S * kStage, kParts = NW * TILE * (OUTS + 1) * 4;
     __shared__ __attribute__((aligned(128))) char lds[kRing > kParts ? kRing : kParts];
     __shared__ int list[TILE];
+    __shared__ unsigned short ids[ROUTED ? kSomeSlots : 1];
+    static_assert(sizeof lds >= (kSortMostExperts + 1) * sizeof(int), "counts");
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l16 = lane & 15, quad = lane >> 4;
     const int jt = (p.n + OUTS - 1) / OUTS;
     const int t = (int)(blockIdx.x / (unsigned)jt), j0 = (int)(blockIdx.x % (unsigned)jt) * OUTS;
     TileOf tile{0, p.rows - t * TILE < TILE ? p.rows - t * TILE : TILE, 0, 0};
+    int slot = 0;                                             // lane i: the tile's i-th
     if constexpr (ROUTED) {
-        tile = routed_tile<TILE>(p, t);
+        const bool counted = !p.sorted && p.rows * p.k > kFewSlots;
+        tile = counted ? counted_tile<TILE, NW * 64>(p, t, (int*)lds, ids, list, slot) : routed_tile<TILE>(p, t);
         if (tile.expert == -2) return;
+        if (!counted) slot = tile_slot(p, tile);            // (of the sorted ones: waited for when the weights are on their way)
     }
-    auto slot_of = [&](int i) { return ROUTED ? list[i] : t * TILE + i; };      // the i-th slot of the tile
     f32x4 acc[MT][JT];
 #pragma unroll
     for (int m = 0; m < MT; m++)
@@ -717,7 +787,9 @@ __global__ __launch_bounds__(NW * 64, (150 * 1024 / (S * NW * ((FORM == kW8H16 ?
         const unsigned char* h = operand<unsigned char>(p.h, p.slots, 1);
         const float* scales = (const float*)(W + (long long)p.experts * p.n * kp) + ((long long)tile.expert * ((p.n + kScaleBlock - 1) / kScaleBlock) + j0 / kScaleBlock) * nb;
         const int hrows = ROUTED && p.per_slot ? p.rows * p.k : p.rows;
-        auto hrow = [&](int i) { const int s = slot_of(i < tile.used ? i : tile.used - 1); return (long long)(ROUTED && !p.per_slot ? s / p.k : s); };
+        // (from the register: a read of LDS would wait for the weights)
+        const int lane_row = ROUTED && !p.per_slot ? slot / p.k : ROUTED ? slot : t * TILE + (lane < tile.used ? lane : tile.used - 1);
+        auto hrow = [&](int i) { return (long long)__shfl(lane_row, i); };
         // lane l of a load takes the 16-byte piece (l & 7) ^ (l >> 3) of row l >> 3 of its eight: fragment reads of eight lanes touch every bank once
         const int piece = (lane & 7) ^ (lane >> 3);
         const unsigned char *hp[MT * 2], *wp[QW], *hs = h;
@@ -778,7 +850,6 @@ __global__ __launch_bounds__(NW * 64, (150 * 1024 / (S * NW * ((FORM == kW8H16 ?
 #pragma unroll
                 for (int b = 0; b < kAhead; b++) if (b < mine_n) issue_weights(way, b, mine + b * kStage, held[kDirect ? 0 : b]);
             }
-            if constexpr (ROUTED) tile_slots<TILE>(p, tile, list);          // (the weights are on their way meanwhile)
 #pragma unroll
             for (int q = 0; q < MT * 2; q++) hp[q] = h + hrow(q * 8 + (lane >> 3)) * hpitch;
             if constexpr (H8) hs = h + hrows * kp + hrow(lane % TILE) * nb4;
@@ -860,9 +931,8 @@ __global__ __launch_bounds__(NW * 64, (150 * 1024 / (S * NW * ((FORM == kW8H16 ?
             if (MT > 1 || JT > 1 || p.cols >= 8) stream(std::integral_constant<int, 1>{});
             else if constexpr (MT == 1 && JT == 1) stream(std::integral_constant<int, 2>{});         // (plan_experts)
         }
-    } else if constexpr (ROUTED) {
-        tile_slots<TILE>(p, tile, list);
     }
+    if (ROUTED && (int)threadIdx.x < TILE) list[threadIdx.x] = slot;
     __syncthreads();                                           // every wave has read its steps
     float* const part = (float*)lds;                           // [NW][TILE][OUTS + 1]
 #pragma unroll
@@ -878,7 +948,7 @@ __global__ __launch_bounds__(NW * 64, (150 * 1024 / (S * NW * ((FORM == kW8H16 ?
         float y = part[m * (OUTS + 1) + c];
 #pragma unroll
         for (int w = 1; w < NW; w++) y += part[(w * TILE + m) * (OUTS + 1) + c];
-        const long long at = (long long)slot_of(m) * p.n + j0 + c;
+        const long long at = (long long)(ROUTED ? list[m] : t * TILE + m) * p.n + j0 + c;
         if (p.out_f32) ((float*)p.out)[at] = y;
         else ((bf16_t*)p.out)[at] = (bf16_t)f32_to_bf16(y);
     }
@@ -1275,7 +1345,7 @@ static bool plan_kernel(int op, int dtype, const Shape& s, Launch* out, Launch* 
             out->fn = routed ? k->routed : k->plain;
             out->block = dim3(k->threads);
         }
-        if (routed && slots > kFewSlots) {
+        if (routed && slots > (fit ? kFewSlots : kSomeSlots)) {
             pre->fn = PG_FN(k_sort_slots);
             pre->arg_bytes = sizeof(ExpertArgs);
             pre->block = dim3(kSortThreads);
