@@ -97,7 +97,7 @@ typedef enum {
  * PG_EXPERT_GEMV  in: W PG_BF16 [inner, n, cols] or PG_F8_WEIGHT of `inner` experts, h, r PG_ROUTED [rows, m]; h [rows, cols], or with
  *                 PG_EXPERT_PER_SLOT [rows, m, cols], PG_BF16 or (with 8-bit W) PG_F8_ROWS; out [rows, m, n], dtype PG_BF16 or PG_F32; m (1 to 64),
  *                 inner = experts (1 to 1024), rows * m < 2^24.  The rows of a slot whose expert is not one of 0 .. inner - 1 are zero.
- *                 With more than 64 slots a dispatch in front lists them by expert in the workspace (also in pg_eager_static's scratch); in a
+ *                 With many slots a dispatch in front lists them by expert in the workspace (also in pg_eager_static's scratch); in a
  *                 captured segment products that go by the same slots share it.
  * PG_EXPERT_SUM   in: z [rows, m, n], r PG_ROUTED [rows, m], and optionally x [rows, n]; dtype of z, x and the output PG_F32 or PG_BF16; rows, n, m (1 to 64).
  *                 Slots are added in order, x behind them, in fp32; an empty slot's z counts as nothing, whatever it holds.  out may be x's buffer.

@@ -642,7 +642,7 @@ __device__ __forceinline__ int tile_slot(const ExpertArgs& p, const TileOf& tile
 }
 // The same for up to kSomeSlots, by the workgroup: the slots of each expert are counted (cnt: experts + 1 places, the last for empty slots), tiles are
 // numbered by expert, and the slots of a tile follow in their order.
-constexpr int kSomeSlots = 256;
+constexpr int kSomeSlots = 512;
 template <int TILE, int THREADS>
 __device__ __forceinline__ TileOf counted_tile(const ExpertArgs& p, int t, int* cnt, unsigned short* ids, int* list, int& slot) {
     constexpr int kEach = kSomeSlots / THREADS;

@@ -370,7 +370,8 @@ def test_layer_of_experts(rows, hidden, width, experts, k, eightbit):
 
 # ------------------------------------------------------------------ lengths, tiles and orders
 @pytest.mark.parametrize("w,h", [("bf16", "bf16"), ("f8", "bf16"), ("f8", "f8")])
-@pytest.mark.parametrize("rows,k,experts,n,cols,out", [(33, 2, 9, 40, 264, "bf16"), (30, 8, 300, 33, 136, "f32"), (9, 20, 3, 300, 520, "bf16"), (9000, 4, 5, 20, 40, "bf16"),
+@pytest.mark.parametrize("rows,k,experts,n,cols,out", [(33, 2, 9, 40, 264, "bf16"), (30, 8, 300, 33, 136, "f32"), (9, 20, 3, 300, 520, "bf16"), (128, 4, 6, 50, 136, "bf16"), (171, 3, 1024, 40, 72, "f32"),
+                                                       (64, 8, 1024, 33, 264, "f32"), (65, 1, 64, 600, 131, "bf16"), (500, 1, 3, 70, 72, "bf16"), (16, 32, 130, 18, 200, "f32"), (9000, 4, 5, 20, 40, "bf16"),
                                                        (700, 60, 1024, 9, 24, "f32"), (1300, 4, 3, 520, 129, "bf16"), (4000, 1, 2, 1030, 72, "f32"), (2500, 2, 40, 700, 65, "bf16")])
 def test_expert_gemv_slots(rows, k, experts, n, cols, out, w, h):
     """Slots on both sides of every bound of the sorting, in small and large tiles."""
@@ -476,11 +477,12 @@ def test_products_by_the_same_slots(rows, k):
     run.close()
 
 
-def test_slots_in_a_buffer_of_the_chain():
+@pytest.mark.parametrize("rows", [50, 300])
+def test_slots_in_a_buffer_of_the_chain(rows):
     """The external list of slots is the chain's own buffer, written between the products: read there when a product runs, except in copy form, which
     reads it when the replay begins."""
-    rows, k, experts, n, cols = 50, 2, 7, 136, 72
-    say("slots in a buffer of the chain")
+    k, experts, n, cols = 2, 7, 136, 72
+    say("slots in a buffer of the chain", rows)
     spec = shared_chain(rows, k, experts, n, cols, True)
     g = torch.Generator().manual_seed(3)
     w = (torch.randn(experts, n, cols, generator=g) * 0.1).to(torch.bfloat16)
@@ -509,10 +511,11 @@ def test_slots_in_a_buffer_of_the_chain():
 
 
 # ------------------------------------------------------------------ other ways in
-def test_static_pass_and_other_streams():
+@pytest.mark.parametrize("rows", [40, 300])
+def test_static_pass_and_other_streams(rows):
     """The layer in the library's own scratch, with lists of sorted slots in it; eagerly on the default device's other streams; two chains at once."""
-    say("static pass, other streams")
-    rows, hidden, width, experts, k = 40, 256, 128, 6, 2
+    say("static pass, other streams", rows)
+    hidden, width, experts, k = 256, 128, 6, 2
     spec, wts, _ = expert_layer(rows, hidden, width, experts, k, True)
     dev = [t.cuda() for t in wts]
     chains = [pg.Chain(spec, dev, "cuda:0") for _ in range(2)]
@@ -549,10 +552,11 @@ def test_static_pass_and_other_streams():
         c.close()
 
 
-def test_a_segment_of_its_own():
+@pytest.mark.parametrize("rows", [50, 270])
+def test_a_segment_of_its_own(rows):
     """The layer in four segments, each in every mode that it has."""
-    say("segments")
-    rows, hidden, width, experts, k = 50, 128, 72, 5, 2
+    say("segments", rows)
+    hidden, width, experts, k = 128, 72, 5, 2
     spec, wts, _ = expert_layer(rows, hidden, width, experts, k, True)
     n = len(spec.kernels)
     ks = [KernelSpec(**{**vars(q), "segment": i * 4 // n}) for i, q in enumerate(spec.kernels)]
