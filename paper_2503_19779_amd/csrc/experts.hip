@@ -20,7 +20,8 @@ template <typename T> __device__ __forceinline__ const T* operand(const void* p,
 __device__ __forceinline__ int up_to(int x, int to) { return (x + to - 1) / to * to; }
 
 // ---- PG_QUANTIZE -------------------------------------------------------------------------------------------
-// 16 lanes take a block of 128 values, 8 each; their maximum goes round in four steps of a DPP row.
+// q = x 2^-e rounded to e4m3 (the one rounding), e the least with max |x| <= 448 * 2^e: the maximum's exponent, and one more above 1.75.  Memory bounds it: each
+// value is read once and written once.  16 lanes take a block of 128 values, 8 each; their maximum goes round in four steps of a DPP row.
 __device__ __forceinline__ float row16_max(float v) {
     v = __builtin_fmaxf(v, dpp_take<0xB1>(v));
     v = __builtin_fmaxf(v, dpp_take<0x4E>(v));
@@ -47,6 +48,7 @@ __device__ __forceinline__ void eight_of(const T* row, int c, int cols, float* f
 }
 
 // 16 lanes take four neighbouring blocks of a row, whose exponents are one word: four loads (eight for fp32) in flight a lane.
+// 8192 rows of 4096 bf16 columns: 21.7 us, 4.66 TB/s (47 us with one block each and narrower loads); a copy of 1 GB reaches 4.8.
 template <typename T>
 __global__ __launch_bounds__(kBlock) void k_quantize(QuantizeArgs p) {
     const T* x = operand<T>(p.x, p.slots, 0);
@@ -97,8 +99,9 @@ __global__ __launch_bounds__(kBlock) void k_quantize(QuantizeArgs p) {
 }
 
 // ---- PG_EXPERT_SUM -----------------------------------------------------------------------------------------
-// A lane takes 16 bytes of a row, with up to eight slots' loads in flight.  A row goes to as many lanes as it has such pieces, rounded up to
-// a power of two, or to several workgroups.
+// fp32 sums, the slots in their order, then x; one rounding at the store.  Memory bounds it.  A lane takes 16 bytes of a row, with up to eight slots' loads in
+// flight.  A row goes to as many lanes as it has such pieces, rounded up to a power of two, or to several workgroups.  4096 rows of 8 slots of 2048 bf16
+// outputs: 31 us, 5.4 TB/s (131 us with one slot's load at a time).
 __host__ __device__ inline int sum_lanes(int pieces) {
     int l = 1;
     while (l < pieces && l < kBlock) l *= 2;
@@ -243,7 +246,9 @@ __device__ __forceinline__ void scores_p(bool sigmoid, double top, double (&x)[N
 
 // A wave takes a row, lane l the experts l * V .. l * V + V - 1.  HIGH: where the choice goes by p itself -- a bias, or sums of two -- p is worked out in
 // fp64; without it the scores are in the order of p, and only the chosen ones need it.  Either way a round of the choice goes by the values rounded to
-// fp32, one instruction a step: what is largest in fp64 is among those that are largest then, mostly the only one.
+// fp32, one instruction a step: what is largest in fp64 is among those that are largest then, mostly the only one.  Each lane keeps its experts sorted, best
+// first, so that a round looks at heads only.  Latency bounds it: a round of the choice is a maximum over the wave and a ballot.  4096 rows, 8 of 256
+// experts by bias and groups: 9.5 us; one row, 8 of 64: the launch, 2.4 us of its 4.1.
 template <typename T, int V, bool HIGH>
 __global__ __launch_bounds__(kBlock) void k_route(RouteArgs p) {
     using K = std::conditional_t<HIGH, double, float>;
@@ -445,7 +450,8 @@ __device__ __forceinline__ int* sorted_order(void* area, int tiles) { return (in
 // One workgroup: a slot's place among its expert's is what a count in LDS says when it is counted, and from the counts follow the places of the
 // experts.  Counts are kept in kCopies for neighbouring lanes to add to (lanes of a wave that add to one place wait for each other: 32768 slots of 64
 // experts 14 us with one).  Slots of an expert come in no fixed order, and a product's rows do not depend on it: each is a row of its own in a tile.
-// Whole tiles come first, so that the small ones fill what is left of the chip at the end.  Bucket `experts` takes the empty slots.
+// Whole tiles come first, so that the small ones fill what is left of the chip at the end.  Bucket `experts` takes the empty slots.  32768 slots of 64
+// experts: 9 us, of which reading the slots through one compute unit and the counting take most; 513 slots: 6.
 __global__ __launch_bounds__(kSortThreads) void k_sort_slots(ExpertArgs p) {
     constexpr int kCopies = 8;
     __shared__ int cnt[kCopies][kSortMostExperts + 1];
@@ -581,6 +587,17 @@ __device__ __forceinline__ f32x4 mfma_bf16(v4u a, v4u b, f32x4 c) {
     return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(v8bf, a), __builtin_bit_cast(v8bf, b), c, 0, 0, 0);
 }
 
+// Sums that the matrix instructions themselves carry over a loop, before their first use behind it: 32 idle cycles, since the compiler was seen to omit the
+// wait states where the last of those instructions and the use lie in different blocks (gemv.hip, mm_drained)
+template <int M, int J>
+__device__ __forceinline__ void sums_drained(f32x4 (&acc)[M][J]) {
+    asm volatile("s_nop 15\n\ts_nop 15" : "+v"(acc[M - 1][J - 1]));
+#pragma unroll
+    for (int m = 0; m < M; m++)
+#pragma unroll
+        for (int j = 0; j < J; j++) asm volatile("" : "+v"(acc[m][j]));
+}
+
 // What the operands are.  8-bit rows go two ways.  The 8-bit matrix instruction lines up the products of eight neighbouring columns with the
 // largest of them and drops what lies below 2^-13 of its binade (found with one large and one small product at every pair of places; between
 // the groups, and onto the accumulator, it adds in fp32): rms 1.5e-5 to 5e-5 of the result, which a bf16 output with its half step of 2^-8 does not
@@ -641,7 +658,8 @@ __device__ __forceinline__ int tile_slot(const ExpertArgs& p, const TileOf& tile
     return lane < tile.used ? slot : __builtin_amdgcn_readlane(slot, tile.used - 1);
 }
 // The same for up to kSomeSlots, by the workgroup: the slots of each expert are counted (cnt: experts + 1 places, the last for empty slots), tiles are
-// numbered by expert, and the slots of a tile follow in their order.
+// numbered by expert, and the slots of a tile follow in their order.  Against the sorting's dispatch, 8 of 64 experts of 2048 columns, 1536 outputs in 8
+// bits: 72 slots 34 -> 27 us, 512 slots 46 -> 42; 1024 slots with 1024 experts' counts 35 -> 56, with bf16 87 -> 90.
 constexpr int kSomeSlots = 512;
 template <int TILE, int THREADS>
 __device__ __forceinline__ TileOf counted_tile(const ExpertArgs& p, int t, int* cnt, unsigned short* ids, int* list, int& slot) {
@@ -751,7 +769,8 @@ template <int N> __device__ __forceinline__ void wait_loads() { asm volatile("s_
 // Products with few rows for an expert, where what bounds it is the way of the weights: a workgroup takes 16 * JT outputs of up to 16 * MT rows of h, its NW
 // waves the steps of K in turn (128 columns; 64 where the weights are bf16), each through a ring of S steps in its own part of LDS, with no barrier
 // until the partial sums meet.  Loads go by whole lines of eight rows, straight into LDS: as fragments in registers, neighbouring lanes took
-// 16 bytes of a row each, and a load the time of 64 lines (64 rows of 4096 columns 16 us for any number of outputs).
+// 16 bytes of a row each, and a load the time of 64 lines (64 rows of 4096 columns 16 us for any number of outputs).  With 8-bit weights 16 rows of 4096
+// columns, 16384 outputs 12.6 us, 5.4 TB/s; 256 slots of 64 experts of 2048 columns, 1536 outputs 37 us, 5.4 TB/s, and 73 in bf16, 5.5 TB/s.
 template <Form FORM, bool ROUTED, int MT, int JT, int S, int NW>
 __global__ __launch_bounds__(NW * 64, (150 * 1024 / (S * NW * ((FORM == kW8H16 ? 2 : 1) * MT + JT) * 2048) > 1 ? 2 : 1) * NW / 4) void k_product(ExpertArgs p) {
     constexpr bool W8 = FORM != kW16H16, H8 = FORM == kW8H8 || FORM == kW8H8Wide;
@@ -932,6 +951,7 @@ __global__ __launch_bounds__(NW * 64, (150 * 1024 / (S * NW * ((FORM == kW8H16 ?
             else if constexpr (MT == 1 && JT == 1) stream(std::integral_constant<int, 2>{});         // (plan_experts)
         }
     }
+    if constexpr (FORM == kW16H16) sums_drained(acc);
     if (ROUTED && (int)threadIdx.x < TILE) list[threadIdx.x] = slot;
     __syncthreads();                                           // every wave has read its steps
     float* const part = (float*)lds;                           // [NW][TILE][OUTS + 1]
@@ -962,7 +982,11 @@ __device__ __forceinline__ unsigned neighbours(unsigned b, unsigned total) {
     return x * each + (x < more ? x : more) + (b >> 3);
 }
 // WR x WJ waves, each RM x JN tiles of 16 rows x 16 outputs, over K in steps of 128 columns (64 where the weights are bf16), S steps in LDS: S - 1 on
-// their way while one is multiplied.
+// their way while one is multiplied.  A block's sum comes from the matrix instruction, times the rows' exponents, and the weights' scale joins it on its way
+// to the fp32 accumulator.  4096 x 4096 x 4096 with both operands in 8 bits: 67 us, 2.04 PFLOP/s of the 2.6 that a large product without scales reaches;
+// the matrix cores are busy 45 % of it.  What bounds it: a step of 256 x 256 takes its fragments through LDS in about the time that it multiplies
+// (256 KB at 128 bytes a clock, 2048 clocks either way), and the two overlap in part; and 16 us before the first step and behind the last, the store of 33 MB
+// among them.  bf16 rows beside 8-bit weights become twice the LDS bytes and half the rate: 130 us, 1.06 PFLOP/s; an fp32 output of 8-bit rows 135 us.
 template <Form FORM, bool ROUTED, int RM, int JN, int WR, int WJ, int S>
 __global__ __launch_bounds__(WR * WJ * 64, 2) void k_product_tile(ExpertArgs p) {
     constexpr bool W8 = FORM != kW16H16, H8 = FORM == kW8H8 || FORM == kW8H8Wide;
@@ -1175,6 +1199,7 @@ __global__ __launch_bounds__(WR * WJ * 64, 2) void k_product_tile(ExpertArgs p) 
         else if constexpr (!(W8 && H8)) stream(std::false_type{});
     }
     // Out by whole pieces of rows: 16 rows of a wave at a time go through its own part of LDS (16 bytes between rows: other banks), 16 bytes a lane from there.
+    if constexpr (FORM == kW16H16) sums_drained(acc);
     __builtin_amdgcn_s_waitcnt(0x0f70);
     __syncthreads();                                           // the last step has been read
     auto emit = [&](auto* out) {
@@ -1237,15 +1262,18 @@ struct TileKernel {
 // The large tiles do the most work to a byte that they load, but a round of them that the chip cannot fill takes as long as a full one.  What a round
 // takes is measured, in us: 8-bit rows and bf16 beside 8-bit weights with 4096 columns, bf16 with 1024.  The cheapest of a form is taken.  4096 outputs:
 // 1024 rows 30 us (8 waves), 2048 rows 41 (4 waves, two workgroups to a compute unit; 56 with 8 waves, 64 with the large tile), 4096 rows 67 (large; 79
-// with 4 waves, 109 with 8).  With fewer workgroups of the smallest tile than kTilesFrom the rows are few, and k_product, which splits K, has more of
-// them: 512 rows (128 workgroups) 20 against 29; slots 26 against 20 (4 of 4 experts for 1133 rows of 768 columns, 512 outputs, 144 workgroups).
+// with 4 waves, 109 with 8).  bf16 slots: 5 of 7 experts for 2000 rows of 1024 columns, 512 outputs 30 (4 waves; 38 with 8), for 4086 rows of 3456 columns,
+// 128 outputs 60 (8 waves; 74 with 4).
 const TileKernel kTileKernels[] = {
     PG_TILE(kW8H8, 4, 8, 4, 2, 2, 67, 0), PG_TILE(kW8H8, 4, 4, 2, 2, 2, 32, 41), PG_TILE(kW8H8, 2, 4, 4, 2, 4, 30, 0),
     PG_TILE(kW8H16, 4, 4, 2, 4, 2, 65, 0), PG_TILE(kW8H16, 2, 4, 4, 2, 3, 45, 0),
     PG_TILE(kW16H16, 4, 8, 4, 2, 2, 36, 0), PG_TILE(kW16H16, 4, 4, 2, 2, 2, 20, 24), PG_TILE(kW16H16, 2, 4, 4, 2, 4, 16, 0),
     PG_TILE(kW8H8Wide, 4, 4, 2, 2, 2, 50, 65), PG_TILE(kW8H8Wide, 2, 4, 4, 2, 4, 48, 0),
 };
-constexpr int kTilesRows = 128;        // of the smallest tile
+// Where an expert's rows do not half fill the smallest tile, or a product makes fewer workgroups of it than this, k_product, which splits K, is faster.  4096 x
+// 4096 in 8 bits, 512 rows (128 workgroups): k_product 20 us, these 29; with bf16 rows 31 and 45.  Routed, 4 of 4 experts for 1133 rows of 768 columns, 512
+// outputs (144 workgroups): 26 and 20.
+constexpr int kTilesRows = 128;
 constexpr long long tiles_from(bool routed, bool eight, bool rows16) { return eight && rows16 ? 256 : routed ? 128 : 192; }
 
 struct RowsKernel {
@@ -1256,12 +1284,16 @@ struct RowsKernel {
 };
 #define PG_ROWS(F, MT, JT, S, NW) {F, PG_FN(k_product<F, false, MT, JT, S, NW>), PG_FN(k_product<F, true, MT, JT, S, NW>), 16 * MT, 16 * JT, NW * 64}
 const RowsKernel kRowsKernels[] = {
+    // MT, JT, S: steps in the ring, as many as leave three workgroups (two beside four tiles of both) room in a compute unit's LDS: more steps with fewer
+    // workgroups are slower (64 slots of 64 experts in 8 bits, two steps of one workgroup 25 us, one step of three 17.5).
     PG_ROWS(kW16H16, 1, 1, 4, 4), PG_ROWS(kW16H16, 1, 2, 2, 4), PG_ROWS(kW16H16, 1, 4, 1, 4), PG_ROWS(kW16H16, 2, 1, 2, 4), PG_ROWS(kW16H16, 2, 2, 2, 4), PG_ROWS(kW16H16, 2, 4, 1, 4), PG_ROWS(kW16H16, 4, 1, 1, 4), PG_ROWS(kW16H16, 4, 2, 1, 4), PG_ROWS(kW16H16, 4, 4, 1, 4),
     PG_ROWS(kW8H16, 1, 1, 3, 4), PG_ROWS(kW8H16, 1, 2, 2, 4), PG_ROWS(kW8H16, 1, 4, 1, 4), PG_ROWS(kW8H16, 2, 1, 1, 4), PG_ROWS(kW8H16, 2, 2, 1, 4), PG_ROWS(kW8H16, 2, 4, 1, 4),
     PG_ROWS(kW8H8, 1, 1, 2, 4), PG_ROWS(kW8H8, 1, 2, 2, 4), PG_ROWS(kW8H8, 1, 4, 1, 4), PG_ROWS(kW8H8, 2, 1, 2, 4), PG_ROWS(kW8H8, 2, 2, 2, 4), PG_ROWS(kW8H8, 2, 4, 1, 4), PG_ROWS(kW8H8, 4, 1, 1, 4), PG_ROWS(kW8H8, 4, 2, 1, 4), PG_ROWS(kW8H8, 4, 4, 1, 4),
     PG_ROWS(kW8H8Wide, 1, 1, 2, 4), PG_ROWS(kW8H8Wide, 1, 2, 2, 4), PG_ROWS(kW8H8Wide, 1, 4, 1, 4), PG_ROWS(kW8H8Wide, 2, 1, 2, 4), PG_ROWS(kW8H8Wide, 2, 2, 2, 4), PG_ROWS(kW8H8Wide, 2, 4, 1, 4), PG_ROWS(kW8H8Wide, 4, 1, 1, 4), PG_ROWS(kW8H8Wide, 4, 2, 1, 4), PG_ROWS(kW8H8Wide, 4, 4, 1, 4),
 };
 
+// Several tiles of outputs share their rows' loads, as long as every compute unit has a workgroup.  4096 x 4096 in 8 bits, 64 rows: 7.4 us with 32 outputs (256
+// workgroups), 8.9 with 16, 9.5 with 64; 512 rows in bf16: 32 us with 64 outputs, 56 with 16.
 constexpr long long kRowsFrom = 256;
 constexpr long long kSmallestTile = 16;
 long long most_tiles(long long slots, long long experts, long long tile) { return slots / tile + std::min(slots, experts + 1); }
@@ -1335,7 +1367,9 @@ static bool plan_kernel(int op, int dtype, const Shape& s, Launch* out, Launch* 
             out->block = dim3(fit->threads);
         } else {
             const long long each = routed ? (3 * slots + 2 * std::min(slots, s.inner) - 1) / (2 * std::min(slots, s.inner)) : slots;      // slots of an expert: half as many again as the mean
-            // the smallest tile that holds an expert's rows, up to 64 of them, with as many outputs as leave kRowsFrom workgroups
+            // The smallest tile that holds an expert's rows, with as many outputs as leave kRowsFrom workgroups.  64 rows where they come in the weights' type:
+            // 16-bit rows beside 8-bit weights take twice the LDS.  In 8 bits 32 are faster up to 128 rows: 64 rows of 4096 x 4096 7.5 and 9.3 us, 128 rows
+            // 9.7 and 10.2, 256 rows 13.9 and 12.9.
             const RowsKernel* k = kRowsKernels;
             const int most = form == kW8H16 || (form != kW16H16 && each <= 128) ? 32 : 64;
             while (k->form != form || (s.cols >= 8 && each > k->rows && k->rows < most)) k++;
