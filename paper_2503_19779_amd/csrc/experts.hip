@@ -1003,12 +1003,28 @@ __global__ __launch_bounds__(WR * WJ * 64, 2) void k_product_tile(ExpertArgs p) 
     __shared__ __attribute__((aligned(16))) char lds_exps[4][H8 ? BM * 4 : 16];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), l16 = lane & 15, quad = lane >> 4;
     const int jt = (p.n + BN - 1) / BN;
-    int t, jb;
+    int t = 0, jb = 0;
     {
-        if (ROUTED) {                                        // each XCD takes two tiles in turn, which mostly are one expert's, with all their outputs
-            const unsigned in = (blockIdx.x >> 3) % (2u * jt);
-            t = (int)((blockIdx.x >> 3) / (2u * jt) * 16 + (blockIdx.x & 7u) * 2 + (in & 1u));
-            jb = (int)(in >> 1);
+        if (ROUTED) {
+            // Sixteen tiles at a time, two to each XCD, which mostly are one expert's, with all their outputs; the last ones, fewer than sixteen, in
+            // stretches like a plain product's.  How many there are at least follows from the slots; the others ask.
+            unsigned b = blockIdx.x, of16 = (unsigned)(p.rows * p.k / BM / 16 * 16) * jt;
+            if (b >= of16) {
+                const int n = p.sorted ? ((const SortedSlots*)p.sorted)->n_tiles : p.tiles;
+                of16 = (unsigned)(n / 16 * 16) * jt;
+                if (b >= (unsigned)n * jt) return;
+                if (b >= of16) {
+                    const unsigned u = neighbours(b - of16, (unsigned)n * jt - of16), pair = u / (2u * jt), in = u % (2u * jt), first = n / 16 * 16 + 2u * pair;
+                    const unsigned two = (unsigned)n - first < 2u ? 1u : 2u;
+                    t = (int)(first + in % two);
+                    jb = (int)(in / two);
+                }
+            }
+            if (b < of16) {
+                const unsigned in = (b >> 3) % (2u * jt);
+                t = (int)((b >> 3) / (2u * jt) * 16 + (b & 7u) * 2 + (in & 1u));
+                jb = (int)(in >> 1);
+            }
         } else {                                             // four tiles of rows, then the next outputs: a stretch is about square
             const unsigned u = neighbours(blockIdx.x, gridDim.x);
             const unsigned group = u / (4u * jt), in = u % (4u * jt), first = 4u * group, rows4 = (unsigned)p.tiles - first < 4u ? (unsigned)p.tiles - first : 4u;
@@ -1272,9 +1288,9 @@ const TileKernel kTileKernels[] = {
 };
 // Where an expert's rows do not half fill the smallest tile, or a product makes fewer workgroups of it than this, k_product, which splits K, is faster.  4096 x
 // 4096 in 8 bits, 512 rows (128 workgroups): k_product 20 us, these 29; with bf16 rows 31 and 45.  Routed, 4 of 4 experts for 1133 rows of 768 columns, 512
-// outputs (144 workgroups): 26 and 20.
+// outputs (144 workgroups): 24 and 19; 2 of 4 for 300 of 2944 columns, 5760 outputs (270) 46 and 37, with an fp32 output 51 and 59.
 constexpr int kTilesRows = 128;
-constexpr long long tiles_from(bool routed, bool eight, bool rows16) { return eight && rows16 ? 256 : routed ? 128 : 192; }
+constexpr long long tiles_from(bool routed, Form form) { return form == kW8H16 ? 256 : !routed ? 192 : form == kW8H8Wide ? 320 : 128; }
 
 struct RowsKernel {
     Form form;
@@ -1339,10 +1355,10 @@ static bool plan_kernel(int op, int dtype, const Shape& s, Launch* out, Launch* 
         const bool routed = op == kExpertGemv, w8 = s.in_dtype[0] == kF8Weight, h8 = s.in_dtype[1] == kF8Rows;
         const long long slots = routed ? s.rows * s.m : s.rows, experts = routed ? s.inner : 1, mean = slots / experts;
         const Form form = !w8 ? kW16H16 : !h8 ? kW8H16 : f32 ? kW8H8Wide : kW8H8;
-        auto with = [&](int tile, int outputs, bool in_pairs = false) {
+        auto with = [&](int tile, int outputs) {
             out->tile = tile;
             out->tiles = (int)(routed ? most_tiles(slots, s.inner, tile) : (slots + tile - 1) / tile);
-            const long long grid = (in_pairs ? (out->tiles + 15) / 16 * 16 : out->tiles) * ((s.n + outputs - 1) / outputs);
+            const long long grid = out->tiles * ((s.n + outputs - 1) / outputs);
             out->grid = dim3((unsigned)grid);
             return grid <= 0x7fffffffll;
         };
@@ -1359,10 +1375,10 @@ static bool plan_kernel(int op, int dtype, const Shape& s, Launch* out, Launch* 
                 if (2 * mean >= k.rows && (!fit || cost < least)) { fit = &k; least = cost; }
                 smallest = wgs;                          // (the last of a form)
             }
-            if (smallest < tiles_from(routed, w8, !h8)) fit = nullptr;
+            if (smallest < tiles_from(routed, form)) fit = nullptr;
         }
         if (fit) {
-            if (!with(fit->rows, fit->outputs, routed)) return false;
+            if (!with(fit->rows, fit->outputs)) return false;
             out->fn = routed ? fit->routed : fit->plain;
             out->block = dim3(fit->threads);
         } else {
