@@ -658,9 +658,10 @@ __device__ __forceinline__ int tile_slot(const ExpertArgs& p, const TileOf& tile
     return lane < tile.used ? slot : __builtin_amdgcn_readlane(slot, tile.used - 1);
 }
 // The same for up to kSomeSlots, by the workgroup: the slots of each expert are counted (cnt: experts + 1 places, the last for empty slots), tiles are
-// numbered by expert, and the slots of a tile follow in their order.  Against the sorting's dispatch, 8 of 64 experts of 2048 columns, 1536 outputs in 8
-// bits: 72 slots 34 -> 27 us, 512 slots 46 -> 42; 1024 slots with 1024 experts' counts 35 -> 56, with bf16 87 -> 90.
-constexpr int kSomeSlots = 512;
+// numbered by expert, and the slots of a tile follow in their order.  Against the sorting's dispatch: 8 of 64 experts of 2048 columns, 1536 outputs in 8
+// bits, 72 slots 34 -> 27 us, 512 slots 46 -> 42; with more than a round of workgroups to count for themselves 1024 slots in bf16 87 -> 90, and with 1024
+// experts' counts 35 -> 56; in one round 1000 slots of 8 experts of 512 columns, 512 outputs 13.4 -> 9.1.
+constexpr int kSomeSlots = 1024;
 template <int TILE, int THREADS>
 __device__ __forceinline__ TileOf counted_tile(const ExpertArgs& p, int t, int* cnt, unsigned short* ids, int* list, int& slot) {
     constexpr int kEach = kSomeSlots / THREADS;
@@ -1395,7 +1396,7 @@ static bool plan_kernel(int op, int dtype, const Shape& s, Launch* out, Launch* 
             out->fn = routed ? k->routed : k->plain;
             out->block = dim3(k->threads);
         }
-        if (routed && slots > (fit ? kFewSlots : kSomeSlots)) {
+        if (routed && slots > (fit ? kFewSlots : out->grid.x <= 2 * kComputeUnits ? kSomeSlots : kSomeSlots / 2)) {       // (half of them where more than a round of workgroups counts)
             pre->fn = PG_FN(k_sort_slots);
             pre->arg_bytes = sizeof(ExpertArgs);
             pre->block = dim3(kSortThreads);
