@@ -1287,10 +1287,14 @@ const TileKernel kTileKernels[] = {
     PG_TILE(kW16H16, 4, 8, 4, 2, 2, 36, 0), PG_TILE(kW16H16, 4, 4, 2, 2, 2, 20, 24), PG_TILE(kW16H16, 2, 4, 4, 2, 4, 16, 0),
     PG_TILE(kW8H8Wide, 4, 4, 2, 2, 2, 50, 65), PG_TILE(kW8H8Wide, 2, 4, 4, 2, 4, 48, 0),
 };
-// Where an expert's rows do not half fill the smallest tile, or a product makes fewer workgroups of it than this, k_product, which splits K, is faster.  4096 x
+// Where an expert has few rows, or a product makes fewer workgroups of the smallest tile than tiles_from, k_product, which splits K, is faster.  8 of 64 experts,
+// 1536 outputs, k_product and these: 8 bits, 36 rows on the mean, 4096 columns 126 and 126 us, 50 rows 157 and 120; bf16, 50 rows 185 and 200, 62 rows 233
+// and 203.  A short K leaves nothing to split: 256 columns, 17 rows 24 and 21 (bf16 beside 8 bits), 50 rows 37 and 24; 1024 columns, 25 rows 40 and 41
+// (in a plain product not: 20 rows of 256 columns, 32768 outputs 5.7 and 6.0).  4096 x
 // 4096 in 8 bits, 512 rows (128 workgroups): k_product 20 us, these 29; with bf16 rows 31 and 45.  Routed, 4 of 4 experts for 1133 rows of 768 columns, 512
 // outputs (144 workgroups): 24 and 19; 2 of 4 for 300 of 2944 columns, 5760 outputs (270) 46 and 37, with an fp32 output 51 and 59.
 constexpr int kTilesRows = 128;
+constexpr long long tiles_mean(bool routed, Form form, long long cols) { return routed && cols <= 512 ? 16 : form == kW16H16 ? 57 : 43; }
 constexpr long long tiles_from(bool routed, Form form) { return form == kW8H16 ? 256 : !routed ? 192 : form == kW8H8Wide ? 320 : 128; }
 
 struct RowsKernel {
@@ -1368,12 +1372,12 @@ static bool plan_kernel(int op, int dtype, const Shape& s, Launch* out, Launch* 
         // (their offsets within a tile, and of gathered rows within h, have 32 bits)
         const long long pitch = w8 ? (s.cols + kScaleBlock - 1) / kScaleBlock * kScaleBlock : 2 * s.cols, hpitch = h8 ? pitch : 2 * s.cols;
         const bool fits = s.cols >= 8 && 256 * std::max(pitch, hpitch) < (1ll << 32) && (!routed || slots * hpitch < (1ll << 32));
-        if (fits && 2 * mean >= kTilesRows) {
+        if (fits && mean >= tiles_mean(routed, form, s.cols)) {
             long long least = 0, smallest = 0;
             for (const TileKernel& k : kTileKernels) {
                 if (k.form != form) continue;
                 const long long wgs = k.workgroups(slots, experts, s.n), cost = k.cost(wgs);
-                if (2 * mean >= k.rows && (!fit || cost < least)) { fit = &k; least = cost; }
+                if ((2 * mean >= k.rows || k.rows == kTilesRows) && (!fit || cost < least)) { fit = &k; least = cost; }
                 smallest = wgs;                          // (the last of a form)
             }
             if (smallest < tiles_from(routed, form)) fit = nullptr;

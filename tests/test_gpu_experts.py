@@ -372,7 +372,8 @@ def test_layer_of_experts(rows, hidden, width, experts, k, eightbit):
 @pytest.mark.parametrize("w,h", [("bf16", "bf16"), ("f8", "bf16"), ("f8", "f8")])
 @pytest.mark.parametrize("rows,k,experts,n,cols,out", [(33, 2, 9, 40, 264, "bf16"), (30, 8, 300, 33, 136, "f32"), (9, 20, 3, 300, 520, "bf16"), (128, 4, 6, 50, 136, "bf16"), (171, 3, 1024, 40, 72, "f32"),
                                                        (64, 8, 1024, 33, 264, "f32"), (65, 1, 64, 600, 131, "bf16"), (500, 1, 3, 70, 72, "bf16"), (16, 32, 130, 18, 200, "f32"),
-                                                       (1000, 1, 16, 30, 72, "bf16"), (256, 4, 5, 40, 40, "f32"), (205, 5, 5, 33, 136, "bf16"), (1000, 1, 60, 70, 264, "bf16"), (9000, 4, 5, 20, 40, "bf16"),
+                                                       (1000, 1, 16, 30, 72, "bf16"), (256, 4, 5, 40, 40, "f32"), (205, 5, 5, 33, 136, "bf16"), (1000, 1, 60, 70, 264, "bf16"),
+                                                       (300, 4, 60, 700, 72, "bf16"), (250, 8, 40, 600, 515, "f32"), (90, 8, 12, 1700, 520, "bf16"), (9000, 4, 5, 20, 40, "bf16"),
                                                        (700, 60, 1024, 9, 24, "f32"), (1300, 4, 3, 520, 129, "bf16"), (4000, 1, 2, 1030, 72, "f32"), (2500, 2, 40, 700, 65, "bf16")])
 def test_expert_gemv_slots(rows, k, experts, n, cols, out, w, h):
     """Slots on both sides of every bound of the sorting, in small and large tiles."""
