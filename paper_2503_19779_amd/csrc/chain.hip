@@ -1261,9 +1261,9 @@ std::vector<Dispatch> segment_dispatches(pg_chain* c, Segment& sg, int kind, int
         return a;
     };
     int n_carry = 0;                      // runs with a carry so far: two places for what they set aside, in turn
-    // The sorted slots that an earlier kernel of the segment left: products that go by the same routed slots, in tiles of one size, sort them once
+    // The sorted slots that an earlier kernel of the segment left: products that go by the same routed slots, in tiles of one size, sort them once --
+    // unless they come by a pointer that the caller gives with the replay, which may lie in a buffer that the chain writes in between.
     std::vector<int> sorted;
-    // -- unless they come by a pointer that the caller gives with the replay, which may lie in a buffer that the chain writes in between.
     auto sorted_before = [&](int ki) -> int {
         const pg_kernel_desc& d = c->k[ki];
         if (d.in[2].kind == PG_REF_EXT && kind != kGraphCopy) return -1;
